@@ -44,7 +44,7 @@
 extern "C" {
 #endif
 
-#define AIS_VERSION 110
+#define AIS_VERSION 120
 
 /* status codes */
 #define AIS_OK                 0
@@ -65,6 +65,7 @@ extern "C" {
                                       and give it a zero row of dH; the batch statistics count it
                                       as a row with lp_train = lp_roll                        */
 #define AIS_FLAG_TIMEOUT      8u   /* a bounded device-side wait ran out; outputs undefined */
+#define AIS_FLAG_PARAM       16u   /* a row's own sampling parameter or random number is out of range: token -1 */
 
 #define AIS_W_VD 0                /* ais_shape.w_layout: W is row-major [V, ldw], one row per vocabulary entry     */
 #define AIS_W_DV 1                /* ais_shape.w_layout: W is row-major [d, ldw], one row per hidden unit          */
@@ -407,6 +408,96 @@ int ais_scatter_words(const void* src, const int32_t* row_index, int64_t n, void
 int ais_logprob_train_static(const ais_shape* shape, const void* H, const void* W, const int32_t* tokens,
                              const uint8_t* mask, float* lp_train, float* lse_train, uint32_t* dev_status,
                              void* stream);
+
+/*
+ * Around on-policy distillation: tokens drawn from logits, a teacher's top logits, and the loss against them.
+ *
+ * The three calls take logits or hidden states of any origin.  A rollout's logits give tokens and their log-probs (the lp_roll of
+ * ais_diagnostics), a teacher's logits give the K entries per row that are worth keeping, and ais_distill trains H and W
+ * towards them without the student's [T, V] logits ever reaching global memory.
+ */
+#define AIS_BF16 0                /* element types of logits */
+#define AIS_F16  1
+#define AIS_F32  2
+#define AIS_LOGITS_MAX_V 327680   /* longest row that ais_sample and ais_top_logits take     */
+#define AIS_TOP_MAX      1024     /* most entries per row of ais_top_logits and ais_distill  */
+#define AIS_MIN_TEMPERATURE 1e-6f
+
+/* How ais_sample filters a row.  A pointer that is not NULL gives one value per row (device memory) and replaces the number. */
+typedef struct ais_sampling {
+    float temperature;              /* 0: the largest entry; otherwise at least AIS_MIN_TEMPERATURE      (1)  */
+    int32_t top_k;                  /* keep the k largest entries; 0 or less: all                        (0)  */
+    float top_p;                    /* of those, the shortest run from the largest down whose probability
+                                       reaches p of theirs; 1 or more: all; the largest stays always     (1)  */
+    float min_p;                    /* of those, the ones with a probability of at least min_p times the
+                                       largest one's; 0 or less: all; at most 1                          (0)  */
+    const float* temperature_rows;
+    const int32_t* top_k_rows;
+    const float* top_p_rows;
+    const float* min_p_rows;
+} ais_sampling;
+void ais_default_sampling(ais_sampling* how);   /* host pointer; fills in the numbers in brackets */
+
+/*
+ * One token per row of logits.  logits [rows, ld] of `dtype` (ld >= V elements; any alignment that the type itself has), u [rows]
+ * uniform random numbers in [0, 1).  Entries of -inf are never drawn.  With e_v = exp((x_v - max x) / temperature) and the kept
+ * set S that the filters leave (order of a row: larger value first, then the smaller index),
+ *     tokens[t] = the smallest index v in S with sum_{w in S, w <= v} e_w > u[t] sum_{w in S} e_w
+ *     lp[t]      = log(e_token / sum_S e)       log-prob under the distribution that was drawn from     (may be NULL)
+ *     lp_full[t] = log(e_token / sum_v e_v)     log-prob at this temperature without the filters        (may be NULL)
+ *     n_kept[t]  = |S|                                                                                  (may be NULL)
+ * Temperature 0 draws the first entry of the order: lp = 0, lp_full at temperature 1.  The sums that decide are exact to about
+ * 1e-12 of their size, whatever the type.  mask [rows] (may be NULL): rows with mask 0 give token -1 and zeros.  So do rows without
+ * a finite entry (AIS_FLAG_EMPTY), with a NaN or +inf (AIS_FLAG_NONFINITE) or with a parameter of their own out of range
+ * (AIS_FLAG_PARAM); the numbers in `how` are checked on the host.
+ * No workspace; results do not depend on the other rows of the call.
+ */
+int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t ld, const ais_sampling* how, const float* u,
+               const uint8_t* mask, int32_t* tokens, float* lp, float* lp_full, int32_t* n_kept, uint32_t* dev_status, void* stream);
+
+/*
+ * The K largest entries of every row of logits in order (larger value first, then the smaller index): ids [rows, ld_out] int32,
+ * values [rows, ld_out] float (the logits themselves), and lse[t] = log sum_v exp(x_v / temperature) (may be NULL).
+ * K <= min(V, AIS_TOP_MAX).  Rows with fewer than K finite entries end in ids -1 and values -inf; rows with mask 0 (mask may be
+ * NULL) hold nothing else and lse 0, rows without a finite entry lse -inf (AIS_FLAG_EMPTY), rows with a NaN or +inf lse NaN
+ * (AIS_FLAG_NONFINITE).  Columns from K on are left alone.  No workspace.
+ */
+int ais_top_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64_t ld, int32_t K, float temperature, const uint8_t* mask,
+                   int32_t* ids, float* values, int64_t ld_out, float* lse, uint32_t* dev_status, void* stream);
+
+/*
+ * Distillation from a teacher's top logits: KL divergence from the teacher's distribution to the student's softmax, summed over the
+ * entries that the teacher gives, and its gradients.  With tau = temperature, x = (H W^T) / tau, p = softmax(x) over the vocabulary,
+ * t_k = logits[t, k] and
+ *     r_k = exp(t_k / tau) / sum_j exp(t_j / tau),
+ *     M   = 1, or with teacher_lse (ais_top_logits at the same temperature): sum_k exp(t_k / tau - teacher_lse[t]), the teacher's
+ *           probability of its own entries
+ *     kl[t] = M sum_k r_k (log r_k + log M - log p_{ids[t, k]}),     loss = sum_t w_t kl[t]
+ *     dH[t,:] = w_t M / tau sum_v (p_v - sum_{k: ids[t,k] = v} r_k) W[v,:]
+ *     dW[v,:] = sum_t w_t M / tau (p_v - sum_{k: ids[t,k] = v} r_k) H[t,:]
+ * w_t = weights[t] (any sign; put tau^2, a mean or an upstream gradient there), or with weights == NULL 1 / (rows with mask 1).
+ * shape: T, d, V, ldh, ldw and w_layout as elsewhere (P, G and fp8_block are not read).
+ * ids [T, ldk] int32, logits [T, ldk] of `dtype`, ldk >= K, K <= AIS_TOP_MAX: any order; entries with a negative id or a logit of -inf
+ * count for nothing, an id beyond V likewise (AIS_FLAG_TOKEN_RANGE), an id given twice counts twice.  Rows with mask 0, without
+ * an entry, or with non-finite teacher or student values (AIS_FLAG_NONFINITE; lse = NaN) give kl 0 and a zero row of dH.
+ * kl [T] float; lse [T] = log sum_v exp(x_v) (may be NULL); loss: one float (may be NULL).
+ * dH [T, ldh] bf16 (may be NULL), dW in W's layout with row stride lddw, bf16 (may be NULL; rounded once from fp32 sums over the
+ * whole batch, which has to fit the workspace).  Without dW the forward pass leaves the exponentials of its logits in scratch rows and
+ * the two tensor-core passes are all there is; dW needs the scratch in its final scale, and the logits are computed a second time.
+ * The tensor cores cut, not round, the partial sums of a contraction, which makes logits a few 1e-6 of their size too small in
+ * the mean (1.6e-8 per 16 terms, measured); the factor 1 / tau carries the correction.
+ */
+#define AIS_DISTILL_DH 1u
+#define AIS_DISTILL_DW 2u
+/* Workspace for the gradients in `grads` (0: the loss alone).  Like the two functions at the top: any size from the minimum on is
+ * accepted, more rows of scratch make fewer passes, neither size falls as T grows; with AIS_DISTILL_DW both are the same.
+ * 0 for an invalid shape. */
+size_t ais_distill_workspace_bytes(const ais_shape* shape, int32_t K, uint32_t grads);
+size_t ais_distill_workspace_min_bytes(const ais_shape* shape, int32_t K, uint32_t grads);
+int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K, const int32_t* ids, const void* logits, int dtype,
+                int64_t ldk, const float* teacher_lse, float temperature, const uint8_t* mask, const float* weights,
+                float* kl, float* lse, float* loss, void* dH, void* dW, int64_t lddw,
+                uint32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

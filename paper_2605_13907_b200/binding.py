@@ -6,6 +6,7 @@ import ctypes as C
 import math
 import operator
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -13,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libais_b200.so")
 _lib = None
 
-FLAG_EMPTY, FLAG_TOKEN_RANGE, FLAG_NONFINITE, FLAG_TIMEOUT = 1, 2, 4, 8
+FLAG_EMPTY, FLAG_TOKEN_RANGE, FLAG_NONFINITE, FLAG_TIMEOUT, FLAG_PARAM = 1, 2, 4, 8, 16
 NUM_MOMENTS = 12
 
 
@@ -41,6 +42,11 @@ class Diag(C.Structure):
 
     def as_dict(self) -> dict:
         return {n: getattr(self, n) for n, _ in self._fields_ if n != "reserved"}
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("temperature_rows", "top_k_rows", "top_p_rows", "min_p_rows")]
 
 
 STAGE_QUANTIZE_H, STAGE_QUANTIZE_W, STAGE_LOGPROB, STAGE_DIAGNOSE, STAGE_LOSS = 1, 2, 4, 8, 16
@@ -113,6 +119,17 @@ def lib() -> C.CDLL:
         L.ais_scatter_words.argtypes = [vp, vp, i64, vp, i64, C.c_uint32, vp]
         L.ais_set_wait_cycles.restype = C.c_int
         L.ais_set_wait_cycles.argtypes = [i64]
+        L.ais_default_sampling.restype = None
+        L.ais_default_sampling.argtypes = [C.POINTER(Sampling)]
+        L.ais_sample.restype = C.c_int
+        L.ais_sample.argtypes = [vp, C.c_int, i64, i64, i64, C.POINTER(Sampling)] + [vp] * 8
+        L.ais_top_logits.restype = C.c_int
+        L.ais_top_logits.argtypes = [vp, C.c_int, i64, i64, i64, C.c_int32, C.c_float, vp, vp, vp, i64, vp, vp, vp]
+        for f in (L.ais_distill_workspace_bytes, L.ais_distill_workspace_min_bytes):
+            f.restype = sz
+            f.argtypes = [C.POINTER(Shape), C.c_int32, C.c_uint32]
+        L.ais_distill.restype = C.c_int
+        L.ais_distill.argtypes = [C.POINTER(Shape), vp, vp, C.c_int32, vp, vp, C.c_int, i64, vp, C.c_float] + [vp] * 7 + [i64, vp, vp, sz, vp]
         L.ais_logprob_train_static.restype = C.c_int
         L.ais_logprob_train_static.argtypes = [C.POINTER(Shape)] + [vp] * 8
         _lib = L
@@ -544,3 +561,191 @@ class AisStep:
 
 _STAGES = (AisStep.quantize_weights, AisStep.forward, AisStep.diagnose, AisStep.backward)
 _STAGE_NAMES = frozenset(("quantize_weights", "forward", "diagnose", "backward"))
+
+
+# ------------------------------------------------------------------ tokens from logits, a teacher's top logits, distillation
+LOGITS_MAX_V, TOP_MAX, MIN_TEMPERATURE = 327680, 1024, 1e-6
+DISTILL_DH, DISTILL_DW = 1, 2
+_LOGIT_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class Sampled(NamedTuple):
+    tokens: torch.Tensor        # [rows] int32; -1: nothing was drawn
+    lp: torch.Tensor            # [rows] float32, log-prob under the distribution drawn from
+    lp_full: torch.Tensor       # [rows] float32, log-prob at the temperature without the filters
+    n_kept: torch.Tensor        # [rows] int32
+
+
+class TopLogits(NamedTuple):
+    ids: torch.Tensor           # [rows, K] int32
+    values: torch.Tensor        # [rows, K] float32
+    lse: torch.Tensor           # [rows] float32
+
+
+def _check_rows(name, t, rows, dtype, device):
+    if t.dim() != 1 or t.numel() != rows or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+        raise AisError(f"{name} must be a contiguous {dtype} tensor of {rows} elements on {device}")
+
+
+def _check_status(status, device):
+    if status is not None and (status.numel() < 1 or status.element_size() != 4 or status.device != device):
+        raise AisError(f"status must be a 32-bit word on {device}")
+
+
+def _check_logits(logits):
+    _require_cuda(logits)
+    if logits.dim() != 2 or logits.dtype not in _LOGIT_TYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise AisError("logits must be [rows, V] bfloat16, float16 or float32 with consecutive columns")
+    rows, V = logits.shape
+    ld = logits.stride(0) if rows > 1 else V
+    if ld < V:
+        raise AisError("rows of the logits overlap")
+    return rows, V, ld
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask: torch.Tensor | None = None,
+           status: torch.Tensor | None = None, out: Sampled | None = None) -> Sampled:
+    """One token per row of `logits` [rows, V] from the uniform numbers `u` [rows] in [0, 1): temperature, then top-k, top-p and min-p
+    (include/ais.h, ais_sample).  Each parameter is a number or a tensor with one value per row (top_k int32, the others float32).
+    `lp` is the log-prob under the distribution drawn from, `lp_full` the one without the filters: with temperature 1 and no filter
+    both are what `diagnostics` takes as lp_roll.  `status` is a 32-bit word that collects FLAG_* bits."""
+    rows, V, ld = _check_logits(logits)
+    dev = logits.device
+    _check_rows("u", u, rows, torch.float32, dev)
+    if mask is not None:
+        _check_rows("mask", mask, rows, torch.uint8, dev)
+    _check_status(status, dev)
+    how = Sampling()
+    for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        if torch.is_tensor(value):
+            _check_rows(name, value, rows, torch.int32 if name == "top_k" else torch.float32, dev)
+            setattr(how, name + "_rows", value.data_ptr())
+        else:
+            setattr(how, name, value)
+    if out is None:
+        f = torch.empty(2, rows, dtype=torch.float32, device=dev)
+        i = torch.empty(2, rows, dtype=torch.int32, device=dev)
+        out = Sampled(i[0], f[0], f[1], i[1])
+    else:
+        for name, t in out._asdict().items():
+            _check_rows("out." + name, t, rows, torch.float32 if name.startswith("lp") else torch.int32, dev)
+    with _on(dev):
+        _check(lib().ais_sample(_ptr(logits), _LOGIT_TYPES[logits.dtype], rows, V, ld, C.byref(how), _ptr(u), _ptr(mask), _ptr(out.tokens),
+                                _ptr(out.lp), _ptr(out.lp_full), _ptr(out.n_kept), _ptr(status), _stream(logits)), "ais_sample")
+    return out
+
+
+def top_logits(logits: torch.Tensor, K: int, temperature: float = 1.0, mask: torch.Tensor | None = None,
+               status: torch.Tensor | None = None, out: TopLogits | None = None) -> TopLogits:
+    """The K largest entries of every row of `logits` [rows, V] in order, their ids, and the row's log-sum-exp at `temperature`
+    (include/ais.h, ais_top_logits): what `DistillStep.step` takes as a teacher."""
+    rows, V, ld = _check_logits(logits)
+    dev = logits.device
+    if mask is not None:
+        _check_rows("mask", mask, rows, torch.uint8, dev)
+    _check_status(status, dev)
+    if out is None:
+        out = TopLogits(torch.empty(rows, K, dtype=torch.int32, device=dev), torch.empty(rows, K, dtype=torch.float32, device=dev),
+                        torch.empty(rows, dtype=torch.float32, device=dev))
+    else:
+        _check_rows("out.lse", out.lse, rows, torch.float32, dev)
+        for name, t, dtype in (("ids", out.ids, torch.int32), ("values", out.values, torch.float32)):
+            if t.shape != (rows, K) or t.dtype != dtype or (K > 1 and t.stride(1) != 1) or t.device != dev or \
+                    (rows > 1 and (t.stride(0) < K or t.stride(0) != out.ids.stride(0))):
+                raise AisError(f"out.{name} must be a {dtype} tensor [{rows}, {K}] on {dev}; ids and values share their row stride")
+    with _on(dev):
+        _check(lib().ais_top_logits(_ptr(logits), _LOGIT_TYPES[logits.dtype], rows, V, ld, K, temperature, _ptr(mask), _ptr(out.ids),
+                                    _ptr(out.values), out.ids.stride(0) if rows > 1 else K, _ptr(out.lse), _ptr(status), _stream(logits)),
+               "ais_top_logits")
+    return out
+
+
+class _on:
+    """The device of the tensors as the current one for the length of a call."""
+
+    def __init__(self, device):
+        self.index, self.back = device.index, None
+
+    def __enter__(self):
+        if self.index is not None and self.index != torch.cuda.current_device():
+            self.back = torch.cuda.current_device()
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
+
+
+def distill_workspace_bytes(shape: Shape, K: int, grads: int) -> int:
+    return int(lib().ais_distill_workspace_bytes(C.byref(shape), K, grads))
+
+
+def distill_workspace_min_bytes(shape: Shape, K: int, grads: int) -> int:
+    return int(lib().ais_distill_workspace_min_bytes(C.byref(shape), K, grads))
+
+
+def distill(shape: Shape, H, W, ids, logits, mask, kl, loss, workspace, temperature: float = 1.0, teacher_lse=None, weights=None, lse=None,
+            dH=None, dW=None, dev_status=None):
+    """KL from a teacher's top logits to the LM head's softmax, and its gradients (include/ais.h, ais_distill); DistillStep keeps the
+    buffers."""
+    _require_cuda(H, W, ids, logits, mask, kl, loss, workspace, teacher_lse, weights, lse, dH, dW, dev_status)
+    T, dev = shape.T, workspace.device
+    K = ids.shape[1] if ids.dim() == 2 else 0
+    if ids.shape != (T, K) or logits.shape != (T, K) or ids.dtype != torch.int32 or logits.dtype not in _LOGIT_TYPES or \
+            (K > 1 and (ids.stride(1) != 1 or logits.stride(1) != 1)) or (T > 1 and ids.stride(0) != logits.stride(0)):
+        raise AisError(f"ids (int32) and logits must be [{T}, K] with consecutive columns and one row stride")
+    head = (shape.d, shape.V) if shape.w_layout == W_DV else (shape.V, shape.d)
+    for name, t, want, ld in (("H", H, (T, shape.d), shape.ldh), ("W", W, head, shape.ldw), ("dH", dH, (T, shape.d), shape.ldh), ("dW", dW, head, None)):
+        if t is not None and (t.shape != want or t.dtype != torch.bfloat16 or t.stride(1) != 1 or (ld is not None and want[0] > 1 and t.stride(0) != ld)):
+            raise AisError(f"{name} must be a bfloat16 tensor {want} with the shape's row stride")
+    for name, t, dtype in (("mask", mask, torch.uint8), ("kl", kl, torch.float32), ("teacher_lse", teacher_lse, torch.float32),
+                           ("weights", weights, torch.float32), ("lse", lse, torch.float32)):
+        if t is not None:
+            _check_rows(name, t, T, dtype, dev)
+    for t in (H, W, ids, logits, loss, dH, dW):
+        if t is not None and t.device != dev:
+            raise AisError("all tensors must live on the workspace's device")
+    _check_status(dev_status, dev)
+    with _on(dev):
+        _check(lib().ais_distill(C.byref(shape), _ptr(H), _ptr(W), K, _ptr(ids), _ptr(logits), _LOGIT_TYPES[logits.dtype],
+                                 ids.stride(0) if T > 1 else K, _ptr(teacher_lse), temperature, _ptr(mask), _ptr(weights), _ptr(kl), _ptr(lse),
+                                 _ptr(loss), _ptr(dH), _ptr(dW), dW.stride(0) if dW is not None else 0, _ptr(dev_status), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream(workspace)), "ais_distill")
+
+
+class DistillStep:
+    """Buffers of a distillation step for a fixed shape: KL per row (`kl`), the weighted sum (`loss`), the student's log-sum-exp
+    (`lse`) and, as wanted, the gradients `dH` and `dW` (bf16, W's layout).  Nothing synchronises."""
+
+    def __init__(self, T: int, d: int, V: int, K: int, temperature: float = 1.0, device="cuda", want_grad: bool = True, want_dw: bool = False,
+                 ldh: int | None = None, ldw: int | None = None, w_layout: int = W_VD, workspace_bytes_cap: int | None = None):
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.K, self.temperature = K, float(temperature)
+        self.shape = make_shape(T, d, V, 1, 1, 128, ldh=ldh, ldw=ldw, w_layout=w_layout)
+        grads = (DISTILL_DH if want_grad else 0) | (DISTILL_DW if want_dw else 0)
+        ws, least = distill_workspace_bytes(self.shape, K, grads), distill_workspace_min_bytes(self.shape, K, grads)
+        if ws == 0:
+            raise AisError("invalid shape, K or gradients")
+        if workspace_bytes_cap is not None and want_grad and not want_dw:
+            # room for every row's scratch in one pass, limited by the cap, never below the minimum
+            ws = max(least, min(least + max(0, (T + 127) // 128 * 128 - 128) * ((V + 63) // 64 * 64) * 2, workspace_bytes_cap))
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=self.device)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        self.kl, self.lse, self.loss = torch.empty(T, **f32), torch.empty(T, **f32), torch.zeros(1, **f32)
+        self.all_rows = torch.ones(T, dtype=torch.uint8, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        bf16 = dict(dtype=torch.bfloat16, device=self.device)
+        self.dH = torch.empty(T, self.shape.ldh, **bf16)[:, :d] if want_grad else None
+        self.dW = torch.empty(d if w_layout == W_DV else V, V if w_layout == W_DV else d, **bf16) if want_dw else None
+
+    def step(self, H, W, ids, logits, teacher_lse=None, mask=None, weights=None) -> None:
+        """H [T, d], W (the LM head), a teacher's `ids` and `logits` [T, K]; with `teacher_lse` [T] (its log-sum-exp at the same
+        temperature) its probabilities are taken as they are, otherwise they are normalised over the K entries.  `weights` [T]:
+        factors of the rows in the loss (default: one over the number of rows whose mask is 1)."""
+        if ids.dim() != 2 or ids.shape[1] != self.K:
+            raise AisError(f"ids must be [{self.shape.T}, {self.K}]")
+        distill(self.shape, H, W, ids, logits, self.all_rows if mask is None else mask, self.kl, self.loss, self.workspace,
+                temperature=self.temperature, teacher_lse=teacher_lse, weights=weights, lse=self.lse, dH=self.dH, dW=self.dW,
+                dev_status=self.status)

@@ -12,7 +12,9 @@
 
 #include "../../include/ais.h"
 #include "host_setup.cuh"
+#include "distill.cuh"
 #include "lmhead.cuh"
+#include "select.cuh"
 #include "stream_kernels.cuh"
 
 namespace ais {
@@ -57,7 +59,7 @@ int device_setup(int* num_sms) {
                 return AIS_ERR_DEVICE;
             g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
         }
-        if (lmhead_prepare() != cudaSuccess || stream_prepare() != cudaSuccess) return AIS_ERR_DEVICE;
+        if (lmhead_prepare() != cudaSuccess || stream_prepare() != cudaSuccess || select_prepare() != cudaSuccess) return AIS_ERR_DEVICE;
         info.num_sms = prop.multiProcessorCount;
         info.ready = true;
     }
@@ -335,6 +337,9 @@ Layout make_layout(const ais_shape* s, const ais_params* p) {
 
 constexpr int64_t kBwdRowsRecommended = 2 * kSms * kBM;
 
+// Distillation: mean relative shortfall of a logit per 16 terms of its contraction (ais_distill in ais.h).
+constexpr double kTruncationPerStep = 1.6e-8;
+
 // Points a pass at its pacing ring.  The passes of a call alternate between two rings: the kernel before the first pass
 // clears both (ring_bytes of them), every later pass finds its own cleared by the one before it (`clears_next`).
 // tiles_per_unit = the largest number of column tiles a unit of the launch walks.  A CTA with only a few announcements to
@@ -357,6 +362,70 @@ int64_t scratch_rows(const Layout& L, int64_t T, size_t workspace_bytes) {
     const int64_t rows = static_cast<int64_t>((workspace_bytes - L.fixed_bytes) / L.u_row_bytes) / kBM * kBM;
     const int64_t t_pad = static_cast<int64_t>(align_up(static_cast<size_t>(T), kBM));
     return rows < t_pad ? rows : t_pad;
+}
+
+// dH = row factor (.) (U W) for the rows of a scratch pass: `a` as for its recompute pass.
+cudaError_t enqueue_dh(LmheadArgs a, const ais_shape* shape, const Layout& L, uint8_t* ws, const CUtensorMap& tmU, const CUtensorMap& tmW_n,
+                       int num_sms, int& pass, cudaStream_t s) {
+    a.tile_active = ws + L.off_flags;
+    a.gate = nullptr;
+    a.ncols = shape->d;
+    a.n_col_tiles = (shape->d + kBN - 1) / kBN;
+    a.n_row_tiles = static_cast<int32_t>((a.rows + kDhRows - 1) / kDhRows);
+    a.nsplit = 1;
+    a.ksteps = (shape->V + 63) / 64;
+    int units = a.n_row_tiles * a.n_col_tiles;
+    const int tail = units % kSms;
+    a.split_from = units;
+    a.ksplit = 1;
+    if (tail > 0) {
+        int ks = L.ksplit > 0 ? L.ksplit : pick_ksplit(tail, a.ksteps, L.split_slots);
+        if (ks > 1 && ks * tail > L.split_slots) ks = L.split_slots / tail;
+        if (ks > 1) {
+            a.split_from = units - tail;
+            a.ksplit = ks;
+            a.part_acc = reinterpret_cast<float*>(ws + L.off_split);
+            units = a.split_from + tail * ks;
+        }
+    }
+    const int ctas = units < num_sms ? units : num_sms;
+    arm_pace(a, ws, L, 1, units, ctas, pass, true);
+    ++pass;
+    const cudaError_t e = launch_lmhead(shape->w_layout == AIS_W_DV ? kBwdDhDv : kBwdDh, tmU, tmW_n, tmU, tmW_n, a, ctas, s);
+    if (e != cudaSuccess || a.ksplit == 1) return e;
+    return launch_dh_reduce(a, s);
+}
+
+// dW (+)= U^T H over the rows of a scratch pass (`mode` kBwdDw or kBwdDwHalf; a.dW or a.dW_half set): both operands are read with the
+// rows as contraction axis; the maps end at a.rows, so rows the scratch still holds from an earlier pass read as zeros
+cudaError_t enqueue_dw(int mode, const LmheadArgs& a, const ais_shape* shape, const Layout& L, uint8_t* ws, const __nv_bfloat16* H, int num_sms,
+                       int& pass, cudaStream_t s) {
+    const bool dv = shape->w_layout == AIS_W_DV;
+    const uint64_t V = static_cast<uint64_t>(shape->V), d = static_cast<uint64_t>(shape->d);
+    CUtensorMap tmU_t, tmH_t;
+    // (the scratch rows are padded to 64 columns; what the padding holds only reaches outputs that are not stored)
+    if (!make_tmap_blocks(&tmU_t, a.U, V, static_cast<uint64_t>(a.rows), L.ldU * 2) ||
+        !make_tmap_blocks(&tmH_t, H, d, static_cast<uint64_t>(a.rows), shape->ldh * 2))
+        return cudaErrorInvalidValue;
+    // output in W's layout: [V, d] = U^T H, or [d, V] = H^T U with the two operands changing places
+    const int out_rows = dv ? shape->d : shape->V, out_cols = dv ? shape->V : shape->d;
+    LmheadArgs w = a;
+    w.rows = out_rows;
+    w.row0 = 0;
+    w.nsplit = 1;
+    w.gate = nullptr;
+    w.tile_active = nullptr;         // it contracts over the rows: nothing to skip
+    w.n_row_tiles = static_cast<int32_t>((out_rows + kDhRows - 1) / kDhRows);
+    w.ncols = out_cols;
+    w.n_col_tiles = (out_cols + kBN - 1) / kBN;
+    w.ksteps = static_cast<int32_t>((a.rows + 63) / 64);
+    const int units = w.n_row_tiles * w.n_col_tiles;
+    const CUtensorMap& tmRow = dv ? tmH_t : tmU_t;
+    const CUtensorMap& tmCol = dv ? tmU_t : tmH_t;
+    const int ctas = units < num_sms ? units : num_sms;
+    arm_pace(w, ws, L, 1, units, ctas, pass, true);
+    ++pass;
+    return launch_lmhead_pair(mode, tmRow, tmCol, tmCol, w, ctas, s);
 }
 
 // What ais_step lets neighbouring stages share: a batch of a few hundred rows is a chain of launches, and these are the ones
@@ -855,62 +924,12 @@ static int loss_bwd(const ais_shape* shape, const ais_params* params, const void
             cudaSuccess)
             return AIS_ERR_DEVICE;
         // dH = c (.) (U W)
-        a.tile_active = ws + L.off_flags;
-        a.gate = nullptr;
-        a.ncols = shape->d;
-        a.n_col_tiles = (shape->d + kBN - 1) / kBN;
-        a.n_row_tiles = static_cast<int32_t>((rows + kDhRows - 1) / kDhRows);
-        a.nsplit = 1;
-        a.ksteps = (shape->V + 63) / 64;
-        units = a.n_row_tiles * a.n_col_tiles;
-        const int tail = units % kSms;
-        a.split_from = units;
-        a.ksplit = 1;
-        if (tail > 0) {
-            int ks = L.ksplit > 0 ? L.ksplit : pick_ksplit(tail, a.ksteps, L.split_slots);
-            if (ks > 1 && ks * tail > L.split_slots) ks = L.split_slots / tail;
-            if (ks > 1) {
-                a.split_from = units - tail;
-                a.ksplit = ks;
-                a.part_acc = reinterpret_cast<float*>(ws + L.off_split);
-                units = a.split_from + tail * ks;
-            }
-        }
-        ctas = units < num_sms ? units : num_sms;
-        arm_pace(a, ws, L, 1, units, ctas, pass, true);
-        ++pass;
-        if (launch_lmhead(dv ? kBwdDhDv : kBwdDh, tmU, tmW_n, tmU, tmW_n, a, ctas, s) != cudaSuccess)
-            return AIS_ERR_DEVICE;
-        if (a.ksplit > 1 && launch_dh_reduce(a, s) != cudaSuccess) return AIS_ERR_DEVICE;
+        if (enqueue_dh(a, shape, L, ws, tmU, tmW_n, num_sms, pass, s) != cudaSuccess) return AIS_ERR_DEVICE;
         if (dW) {
-            // dW (+)= U^T H over the rows of this pass: both operands are read with the rows as contraction axis;
-            // the maps end at `rows`, so rows the scratch still holds from an earlier pass read as zeros
-            CUtensorMap tmU_t, tmH_t;
-            // (the scratch rows are padded to 64 columns; what the padding holds only reaches outputs that are not stored)
-            if (!make_tmap_blocks(&tmU_t, U, V, static_cast<uint64_t>(rows), L.ldU * 2) ||
-                !make_tmap_blocks(&tmH_t, Hc, d, static_cast<uint64_t>(rows), shape->ldh * 2))
-                return AIS_ERR_DEVICE;
-            // output in W's layout: [V, d] = U^T H, or [d, V] = H^T U with the two operands changing places
-            const int out_rows = dv ? shape->d : shape->V, out_cols = dv ? shape->V : shape->d;
-            LmheadArgs w = a;
-            w.rows = out_rows;
-            w.row0 = 0;
-            w.tile_active = nullptr;         // it contracts over the rows: nothing to skip
-            w.n_row_tiles = static_cast<int32_t>((out_rows + kDhRows - 1) / kDhRows);
-            w.ncols = out_cols;
-            w.n_col_tiles = (out_cols + kBN - 1) / kBN;
-            w.ksteps = static_cast<int32_t>((rows + 63) / 64);
-            w.dW = dW;
-            w.lddw = lddw;
-            w.dw_accumulate = (dw_accumulate || r0 > 0) ? 1 : 0;
-            units = w.n_row_tiles * w.n_col_tiles;
-            const CUtensorMap& tmRow = dv ? tmH_t : tmU_t;
-            const CUtensorMap& tmCol = dv ? tmU_t : tmH_t;
-            ctas = units < num_sms ? units : num_sms;
-            arm_pace(w, ws, L, 1, units, ctas, pass, true);
-            ++pass;
-            if (launch_lmhead_pair(kBwdDw, tmRow, tmCol, tmCol, w, ctas, s) != cudaSuccess)
-                return AIS_ERR_DEVICE;
+            a.dW = dW;
+            a.lddw = lddw;
+            a.dw_accumulate = (dw_accumulate || r0 > 0) ? 1 : 0;
+            if (enqueue_dw(kBwdDw, a, shape, L, ws, Hc, num_sms, pass, s) != cudaSuccess) return AIS_ERR_DEVICE;
         }
     }
     return AIS_OK;
@@ -1012,6 +1031,254 @@ int ais_step(const ais_shape* shape, const ais_params* params, const ais_step_ar
                       a->adv, a->w_tilde, a->dH, a->loss, a->diag, a->dW, a->lddw, static_cast<int>(a->dw_accumulate), a->dev_status,
                       a->workspace, a->workspace_bytes, stream, fuse);
     return st;
+}
+
+// ---------------------------------------------------------------------------------------------- distillation
+namespace {
+
+struct DistillLayout : Layout {
+    size_t off_counters, clear_bytes;                          // pacing rings, counters and redo flags: cleared by the opening launch
+    size_t off_ids, off_logits, off_pick;                      // [T][K]
+    size_t off_lse, off_partials, off_hidden;
+};
+
+int check_distill_shape(const ais_shape* s, int32_t K, uint32_t grads) {
+    if (!s) return AIS_ERR_NULL;
+    ais_shape own = *s;                                        // the fields that distillation does not read
+    own.P = own.G = 1;
+    own.P_total = 0;
+    own.fp8_block = 128;
+    const int st = check_shape(&own);
+    if (st != AIS_OK) return st;
+    if (K <= 0 || K > s->V || (grads & ~(AIS_DISTILL_DH | AIS_DISTILL_DW)) != 0) return AIS_ERR_SHAPE;
+    return K > AIS_TOP_MAX ? AIS_ERR_LIMIT : AIS_OK;
+}
+
+DistillLayout compute_distill_layout(const ais_shape* s, int32_t K, uint32_t grads) {
+    DistillLayout L = {};
+    const size_t T = static_cast<size_t>(s->T > 0 ? s->T : 1);
+    L.t_ld = static_cast<int64_t>(align_up(T, 64));
+    L.train = plan_pass(s->T, s->V, s->d, kMaxRanges, 0);
+    const int64_t one = most_range_rows(kTileOne, s->T, s->V, s->d, kMaxRanges, 0), two = most_range_rows(kTileTwo, s->T, s->V, s->d, kMaxRanges, 0);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += align_up(bytes, 256);
+        return at;
+    };
+    L.part_bytes = align_up(2 * static_cast<size_t>(one > two ? one : two) * sizeof(float), 256);
+    L.off_part[0] = take(3 * L.part_bytes);
+    L.off_flags = take(static_cast<size_t>(L.t_ld / kBM + 2));
+    L.off_pace = take(2 * kPaceRingBytes);
+    L.off_counters = take(256);
+    L.off_redo = take(static_cast<size_t>(L.t_ld / kBM + 2));
+    L.clear_bytes = off - L.off_pace;
+    L.off_coef = take(L.t_ld * sizeof(float));
+    L.off_scale = take(L.t_ld * sizeof(float));
+    L.off_lse = take(L.t_ld * sizeof(float));
+    L.off_partials = take((T + kDistillRows - 1) / kDistillRows * sizeof(double));
+    L.off_ids = take(T * K * sizeof(int32_t));
+    L.off_logits = take(T * K * sizeof(float));
+    L.off_pick = take(T * K * sizeof(float));
+    L.ldU = static_cast<int64_t>(align_up(static_cast<size_t>(s->V), 64));
+    L.u_row_bytes = static_cast<size_t>(L.ldU) * sizeof(__nv_bfloat16);
+    if (grads & AIS_DISTILL_DW) L.off_hidden = take(T * static_cast<size_t>(s->ldh) * sizeof(__nv_bfloat16));
+    if (grads & AIS_DISTILL_DH) {
+        const int64_t tiles = ((s->T + kDhRows - 1) / kDhRows) * ((s->d + kBN - 1) / kBN);
+        const int ksteps = (s->V + 63) / 64;
+        L.split_slots = most_split_slots(tiles, ksteps);
+        L.ksplit = tiles >= kSms ? 0 : tiles > 0 ? pick_ksplit(static_cast<int>(tiles), ksteps, L.split_slots) : 1;
+        L.off_split = take(static_cast<size_t>(L.split_slots) * kPartTileFloats * sizeof(float));
+    }
+    L.off_u = off;
+    L.fixed_bytes = off;
+    return L;
+}
+
+// As make_layout: the last one of each thread.
+DistillLayout distill_layout(const ais_shape* s, int32_t K, uint32_t grads) {
+    struct Key {
+        int64_t T, ldh;
+        int32_t d, V, K;
+        uint32_t grads;
+    };
+    static thread_local Key key = {-1, 0, 0, 0, 0, 0};
+    static thread_local DistillLayout layout;
+    if (key.T != s->T || key.ldh != s->ldh || key.d != s->d || key.V != s->V || key.K != K || key.grads != grads) {
+        layout = compute_distill_layout(s, K, grads);
+        key = {s->T, s->ldh, s->d, s->V, K, grads};
+    }
+    return layout;
+}
+
+size_t distill_bytes(const ais_shape* s, int32_t K, uint32_t grads, bool least) {
+    if (check_distill_shape(s, K, grads) != AIS_OK) return 0;
+    const DistillLayout L = distill_layout(s, K, grads);
+    if (grads == 0) return L.fixed_bytes;
+    int64_t rows = static_cast<int64_t>(align_up(static_cast<size_t>(s->T > 0 ? s->T : 1), kBM));
+    if (!(grads & AIS_DISTILL_DW)) {
+        if (least) rows = kBM;
+        else if (rows > kBwdRowsRecommended) rows = kBwdRowsRecommended;
+    }
+    return L.fixed_bytes + static_cast<size_t>(rows) * L.u_row_bytes;
+}
+
+}  // namespace
+
+size_t ais_distill_workspace_bytes(const ais_shape* shape, int32_t K, uint32_t grads) { return distill_bytes(shape, K, grads, false); }
+size_t ais_distill_workspace_min_bytes(const ais_shape* shape, int32_t K, uint32_t grads) { return distill_bytes(shape, K, grads, true); }
+
+int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K, const int32_t* ids, const void* logits, int dtype,
+                int64_t ldk, const float* teacher_lse, float temperature, const uint8_t* mask, const float* weights, float* kl, float* lse,
+                float* loss, void* dH, void* dW, int64_t lddw, uint32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream) {
+    const uint32_t grads = (dH ? AIS_DISTILL_DH : 0u) | (dW ? AIS_DISTILL_DW : 0u);
+    int st = check_distill_shape(shape, K, grads);
+    if (st != AIS_OK) return st;
+    const int64_t T = shape->T;
+    const uint64_t V = static_cast<uint64_t>(shape->V), d = static_cast<uint64_t>(shape->d);
+    const bool dv = shape->w_layout == AIS_W_DV;
+    if (dtype != AIS_BF16 && dtype != AIS_F16 && dtype != AIS_F32) return AIS_ERR_PARAM;
+    if (!(temperature >= AIS_MIN_TEMPERATURE && temperature < INFINITY)) return AIS_ERR_PARAM;
+    if (ldk < K) return AIS_ERR_SHAPE;
+    if (!W || (T > 0 && (!H || !ids || !logits || !mask || !kl))) return AIS_ERR_NULL;
+    if (!aligned(H, 16) || !aligned(W, 16) || !aligned(dH, 16) || !aligned(dW, 16) || !aligned(ids, 4) || !aligned(logits, dtype == AIS_F32 ? 4 : 2))
+        return AIS_ERR_ALIGN;
+    if (dW && lddw < static_cast<int64_t>(dv ? V : d)) return AIS_ERR_SHAPE;
+    if (dW && lddw % 8 != 0) return AIS_ERR_ALIGN;
+    const DistillLayout L = distill_layout(shape, K, grads);
+    const size_t scratch_min = grads == 0 ? 0 : (dW ? align_up(static_cast<size_t>(T > 0 ? T : 1), kBM) : static_cast<size_t>(kBM)) * L.u_row_bytes;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < L.fixed_bytes + scratch_min) return AIS_ERR_WORKSPACE;
+    int num_sms = 0;
+    st = device_setup(&num_sms);
+    if (st != AIS_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (loss && cudaMemsetAsync(loss, 0, sizeof(float), s) != cudaSuccess) return AIS_ERR_DEVICE;
+        if (dW && cudaMemset2DAsync(dW, lddw * 2, 0, (dv ? V : d) * 2, dv ? d : V, s) != cudaSuccess) return AIS_ERR_DEVICE;
+        return AIS_OK;
+    }
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    uint32_t* counters = reinterpret_cast<uint32_t*>(ws + L.off_counters);       // rows of the batch, rows to recompute, ticket
+    int32_t* sorted_ids = reinterpret_cast<int32_t*>(ws + L.off_ids);
+    float* pick = reinterpret_cast<float*>(ws + L.off_pick);
+    __nv_bfloat16* U = reinterpret_cast<__nv_bfloat16*>(ws + L.off_u);
+    const bool keep = dH && !dW;                                 // the forward pass leaves the exponentials for the dH pass
+    const int64_t blk_rows = grads == 0 ? T : scratch_rows(L, T, workspace_bytes);
+
+    const FlagsJob flags = {mask, T, ws + L.off_flags, ws + L.off_pace, static_cast<int64_t>(L.clear_bytes), AdvJob{}};
+    const TeacherJob teacher = {ids, logits, dtype, ldk, K, shape->V, T, mask, sorted_ids, reinterpret_cast<float*>(ws + L.off_logits), counters, dev_status};
+    CUtensorMap tmW_k, tmW_n, tmW_tail, tmU;                     // as in loss_bwd
+    if (!(dv ? make_tmap_blocks(&tmW_k, W, whole_blocks(V), d, shape->ldw * 2) &&
+                   make_tmap(&tmW_tail, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, W, V, d, shape->ldw * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B)
+             : make_tmap(&tmW_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, W, d, V, shape->ldw * 2, 64, kBN, CU_TENSOR_MAP_SWIZZLE_128B)))
+        return AIS_ERR_DEVICE;
+    if (dH && (!(dv ? make_tmap(&tmW_n, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, W, V, d, shape->ldw * 2, 64, kBN, CU_TENSOR_MAP_SWIZZLE_128B)
+                    : make_tmap_blocks(&tmW_n, W, d, V, shape->ldw * 2)) ||
+               !make_tmap(&tmU, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, U, V, static_cast<uint64_t>(blk_rows), L.ldU * 2, 64, kBM, CU_TENSOR_MAP_SWIZZLE_128B)))
+        return AIS_ERR_DEVICE;
+    if (launch_flags(flags, s) != cudaSuccess || launch_teacher(teacher, s) != cudaSuccess) return AIS_ERR_DEVICE;
+
+    DistillJob job = {};
+    job.K = K;
+    job.V = shape->V;
+    job.inv_tau = 1.0 / static_cast<double>(temperature);
+    job.mask = mask;
+    job.ids = sorted_ids;
+    job.logits = teacher.sorted_logits;
+    job.pick = pick;
+    job.teacher_lse = teacher_lse;
+    job.weights = weights;
+    job.n_valid = counters;
+    job.kl = kl;
+    job.lse = lse;
+    job.row_lse = reinterpret_cast<float*>(ws + L.off_lse);
+    job.coef = reinterpret_cast<float*>(ws + L.off_coef);
+    job.scale = keep ? reinterpret_cast<float*>(ws + L.off_scale) : nullptr;
+    job.U = keep ? U : nullptr;
+    job.ldU = L.ldU;
+    job.redo_flags = ws + L.off_redo;
+    job.redo_count = counters + 1;
+    job.partials = reinterpret_cast<double*>(ws + L.off_partials);
+    job.n_partials = static_cast<int32_t>((T + kDistillRows - 1) / kDistillRows);
+    job.ticket = counters + 2;
+    job.loss = loss;
+    job.status = dev_status;
+
+    int pass = 0;                                                // tensor-core launches so far
+    for (int64_t r0 = 0; r0 < T; r0 += blk_rows) {
+        const int64_t rows = T - r0 < blk_rows ? T - r0 : blk_rows;
+        const __nv_bfloat16* Hc = static_cast<const __nv_bfloat16*>(H) + r0 * shape->ldh;
+        const PassPlan plan = rows == T ? L.train : plan_pass(rows, shape->V, shape->d, kMaxRanges, 0);
+        CUtensorMap tmH;
+        if (!make_tmap(&tmH, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, Hc, d, static_cast<uint64_t>(rows), shape->ldh * 2, 64, plan.unit_rows,
+                       CU_TENSOR_MAP_SWIZZLE_128B))
+            return AIS_ERR_DEVICE;
+        LmheadArgs a;
+        memset(&a, 0, sizeof(a));
+        a.wait_cycles = wait_cycles();
+        a.rows = rows;
+        a.row0 = r0;
+        a.mask = mask;
+        a.ncols = shape->V;
+        a.n_col_tiles = (shape->V + kBN - 1) / kBN;
+        a.n_row_tiles = static_cast<int32_t>((rows + plan.unit_rows - 1) / plan.unit_rows);
+        a.nsplit = plan.ranges;
+        a.ksteps = shape->d / 64;
+        a.block_tiles = shape->V / kBN;
+        a.sgroups = 1;
+        a.part_ld = static_cast<int64_t>(align_up(static_cast<size_t>(rows), 64));
+        a.part_m = reinterpret_cast<float*>(ws + L.off_part[0]) - r0;             // (indexed by the row of the batch)
+        a.part_s = a.part_m + L.part_bytes / sizeof(float);
+        a.part_z = a.part_s + L.part_bytes / sizeof(float);
+        a.U = U;
+        a.ldU = L.ldU;
+        a.keep_rows = keep ? rows : 0;
+        a.x_scale = static_cast<float>(job.inv_tau * (1.0 + kTruncationPerStep * (shape->d / 16)));
+        a.picks = K;
+        a.pick_ids = sorted_ids;
+        a.pick_x = pick;
+        a.status = dev_status;
+        a.tile_active = ws + L.off_flags;
+        const int units = a.n_row_tiles * a.nsplit, ctas = units < num_sms ? units : num_sms;
+        const CUtensorMap& tail_map = dv ? tmW_tail : tmH;
+        auto logits_pass = [&](int mode) {
+            arm_pace(a, ws, L, (a.n_col_tiles + a.nsplit - 1) / a.nsplit, units, ctas, pass, pass > 0);
+            ++pass;
+            return plan.two ? launch_lmhead_pair(mode, tmH, tmW_k, tail_map, a, ctas, s) : launch_lmhead(mode, tmH, tmW_k, tail_map, tmW_k, a, ctas, s);
+        };
+        if (logits_pass(keep ? (dv ? kFwdPickKeepDv : kFwdPickKeep) : dv ? kFwdPickDv : kFwdPick) != cudaSuccess) return AIS_ERR_DEVICE;
+        job.row0 = r0;
+        job.rows = rows;
+        job.part_m = a.part_m;
+        job.part_s = a.part_s;
+        job.nparts = plan.parts();
+        job.part_ld = a.part_ld;
+        if (launch_distill_rows(job, s) != cudaSuccess) return AIS_ERR_DEVICE;
+        if (grads == 0) continue;
+        // the scratch in plain form (for dW), or only the rows that the exponent form does not reach (a gate that is usually closed)
+        a.lse = job.row_lse;
+        a.coef = job.coef;
+        a.row_scale = job.scale;
+        if (keep) {
+            a.tile_active = ws + L.off_redo;
+            a.gate = job.redo_count;
+        }
+        if (logits_pass(dv ? kBwdPPickDv : kBwdPPick) != cudaSuccess) return AIS_ERR_DEVICE;
+        if (dH) {
+            a.dH = static_cast<__nv_bfloat16*>(dH);
+            a.lddh = shape->ldh;
+            if (enqueue_dh(a, shape, L, ws, tmU, tmW_n, num_sms, pass, s) != cudaSuccess) return AIS_ERR_DEVICE;
+        }
+        if (dW) {
+            // rows without a gradient may hold anything, and 0 x NaN is NaN: the contraction over the rows reads a copy without them
+            __nv_bfloat16* rows_of = reinterpret_cast<__nv_bfloat16*>(ws + L.off_hidden);
+            if (launch_live_rows(Hc, shape->ldh, rows, shape->d, job.coef, rows_of, s) != cudaSuccess) return AIS_ERR_DEVICE;
+            a.dW_half = dW;
+            a.lddw = lddw;
+            if (enqueue_dw(kBwdDwHalf, a, shape, L, ws, rows_of, num_sms, pass, s) != cudaSuccess) return AIS_ERR_DEVICE;
+        }
+    }
+    return AIS_OK;
 }
 
 }  // extern "C"

@@ -356,6 +356,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 continue;
             }
             RowState r = begin_row<MODE>(a, static_cast<int64_t>(w.rt) * kBM + r_in_tile, flags);
+            if (pick_mode(MODE)) pick_start(a, r, w.t0 * kBN + half * 128);
             const bool store = r.in && (BASE == kBwdP || r.lrow < a.keep_rows);
             const float tscale = (MODE == kFwdFp8T) ? (*a.scale_a) * (*a.scale_b) : 1.f;
             for (int t = w.t0; t < w.t1 && ok; ++t) {
@@ -497,6 +498,12 @@ cudaError_t launch_lmhead(int mode, const CUtensorMap& tmA, const CUtensorMap& t
         case kBwdDhDv:   return launch_mode<kBwdDhDv>(tmA, tmB, tmSA, args, num_ctas, stream);
         case kFwdKeep:   return launch_mode<kFwdKeep>(tmA, tmB, tmSA, args, num_ctas, stream);
         case kFwdKeepDv: return launch_mode<kFwdKeepDv>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPick: return launch_mode<kFwdPick>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPickDv: return launch_mode<kFwdPickDv>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPickKeep: return launch_mode<kFwdPickKeep>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPickKeepDv: return launch_mode<kFwdPickKeepDv>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kBwdPPick: return launch_mode<kBwdPPick>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kBwdPPickDv: return launch_mode<kBwdPPickDv>(tmA, tmB, tmSA, args, num_ctas, stream);
     }
     return cudaErrorInvalidValue;
 }
@@ -510,7 +517,8 @@ cudaError_t lmhead_prepare() {
     const cudaError_t all[] = {lmhead_fp8_block_prepare(), lmhead_pair_prepare(), prepare_mode<kFwdBf16>(), prepare_mode<kBwdP>(), prepare_mode<kBwdDh>(),
                                prepare_mode<kFwdFp8T>(), prepare_mode<kFwdMx>(), prepare_mode<kFwdMx4>(),
                                prepare_mode<kFwdBf16Dv>(), prepare_mode<kBwdPDv>(), prepare_mode<kBwdDhDv>(), prepare_mode<kFwdKeep>(),
-                               prepare_mode<kFwdKeepDv>()};
+                               prepare_mode<kFwdKeepDv>(), prepare_mode<kFwdPick>(), prepare_mode<kFwdPickDv>(), prepare_mode<kFwdPickKeep>(),
+                               prepare_mode<kFwdPickKeepDv>(), prepare_mode<kBwdPPick>(), prepare_mode<kBwdPPickDv>()};
     for (const cudaError_t e : all)
         if (e != cudaSuccess) return e;
     return cudaSuccess;

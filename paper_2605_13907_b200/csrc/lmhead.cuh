@@ -24,16 +24,33 @@ enum LmheadMode : int {
     kBwdDhDv   = 10,
     // the trainer pass that also stores the exponentials of its logits in the scratch of the dH pass (see exp_form)
     kFwdKeep   = 11,
-    kFwdKeepDv = 12
+    kFwdKeepDv = 12,
+    // distillation: logits scaled by LmheadArgs::x_scale; a list of columns per row (ascending) instead of one target.  The forward
+    // passes leave the scaled logits of the listed columns behind, the recompute pass puts given values at them
+    kFwdPick       = 13,
+    kFwdPickDv     = 14,
+    kFwdPickKeep   = 15,
+    kFwdPickKeepDv = 16,
+    kBwdPPick      = 17,
+    kBwdPPickDv    = 18,
+    // the dW pass with a bf16 result
+    kBwdDwHalf     = 19
 };
 
 // What a mode computes (its epilogue and work-unit shape), whatever the layout of W.
 __host__ __device__ constexpr int base_mode(int mode) {
-    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv ? kFwdBf16 : mode == kBwdPDv ? kBwdP : mode == kBwdDhDv ? kBwdDh : mode;
+    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv || (mode >= kFwdPick && mode <= kFwdPickKeepDv) ? kFwdBf16
+           : mode == kBwdPDv || mode == kBwdPPick || mode == kBwdPPickDv                                                ? kBwdP
+           : mode == kBwdDhDv                                                                                           ? kBwdDh
+           : mode == kBwdDwHalf                                                                                         ? kBwdDw
+                                                                                                                        : mode;
 }
+// The passes of the distillation.
+__host__ __device__ constexpr bool pick_mode(int mode) { return mode >= kFwdPick && mode <= kBwdPPickDv; }
 // B operand stored with the output column as the contiguous axis (MN-major)?
 __host__ __device__ constexpr bool b_mn_major(int mode) {
-    return mode == kBwdDh || mode == kBwdDw || mode == kFwdBf16Dv || mode == kBwdPDv || mode == kFwdKeepDv;
+    return mode == kBwdDh || mode == kBwdDw || mode == kBwdDwHalf || mode == kFwdBf16Dv || mode == kBwdPDv || mode == kFwdKeepDv ||
+           mode == kFwdPickDv || mode == kFwdPickKeepDv || mode == kBwdPPickDv;
 }
 
 constexpr int kSms = 148;                // SMs of the part; the work splits below are planned for it
@@ -128,6 +145,11 @@ struct LmheadArgs {
     uint32_t* pace_clear;  // ring of the next pass of the same call, cleared by this one; NULL = nothing to clear
     int32_t overlap;       // the pass needs nothing from the kernel before it (the other pass of the same call): it starts
                            // while that one drains and waits for it only at its own end
+    float x_scale;         // distillation: factor of the logits
+    int32_t picks;         // listed columns per row
+    const int32_t* pick_ids;   // [rows of the batch][picks], ascending
+    float* pick_x;         // the same shape: scaled logits of the listed columns (forward), scratch values at them (recompute)
+    void* dW_half;         // dW pass with a bf16 result, row stride lddw
     int32_t pace_per_unit; // announcements per unit = ceil(largest number of stage fills of a unit / fills per announcement)
 };
 

@@ -194,7 +194,7 @@ __device__ __forceinline__ void leave_pass(const LmheadArgs& a) {
 // (log2-domain running reference, sum of 2^(z log2e - reference), target logit).
 // Recompute: U = mul (e^(z - off) - onehot) in plain form (off = lse, mul = c), mul = 1, off = 0 and `target` at the target
 // column in exponent form (exp_form).
-constexpr __host__ __device__ bool keep_mode(int mode) { return mode == kFwdKeep || mode == kFwdKeepDv; }
+constexpr __host__ __device__ bool keep_mode(int mode) { return mode == kFwdKeep || mode == kFwdKeepDv || mode == kFwdPickKeep || mode == kFwdPickKeepDv; }
 // |reference| (log2 units) up to which the kept exponentials are relative to 0; just above exp_form's largest lse
 constexpr float kKeepRange = 86.0f;
 
@@ -205,6 +205,7 @@ struct RowState {
     float m2, s, zy;
     float off2, mul, target;
     bool ef;
+    int pick, next;                  // distillation: position in the row's list, the column that stands there
 };
 
 template <int MODE>
@@ -221,19 +222,55 @@ __device__ __forceinline__ RowState begin_row(const LmheadArgs& a, int64_t lrow,
     r.zy = -INFINITY;
     r.off2 = r.mul = r.target = 0.f;
     r.ef = false;
+    r.pick = 0;
+    r.next = INT32_MAX;
     if (!r.in) return r;
-    r.y = a.tokens[r.grow];
+    if (!pick_mode(MODE)) r.y = a.tokens[r.grow];
     r.valid = a.mask[r.grow] != 0;
-    if (r.valid && (r.y < 0 || r.y >= a.ncols)) { flags |= AIS_FLAG_TOKEN_RANGE; r.y = -1; }
+    if (!pick_mode(MODE) && r.valid && (r.y < 0 || r.y >= a.ncols)) { flags |= AIS_FLAG_TOKEN_RANGE; r.y = -1; }
     if (BASE == kBwdP) {
         const float lse = a.lse[r.grow];
         r.mul = a.coef[r.grow];
         if (r.mul == 0.f) r.valid = false;             // rows without gradient are written as exact zeros
         r.ef = a.row_scale != nullptr && exp_form(lse);
-        if (r.ef) { r.mul = 1.f; r.target = exp_form_target(a.lp[r.grow], lse); }
+        if (r.ef) { r.mul = 1.f; r.target = pick_mode(MODE) ? 0.f : exp_form_target(a.lp[r.grow], lse); }
         else r.off2 = lse * kLog2e;
     }
     return r;
+}
+
+// Distillation: the first listed column of the row from `col` on.  The list is short and ascending, so a thread walks it along with
+// its columns and compares one number per slice of 32.
+__device__ __forceinline__ void pick_start(const LmheadArgs& a, RowState& r, int col) {
+    if (!r.in || !r.valid) return;
+    const int32_t* ids = a.pick_ids + r.grow * a.picks;
+    int lo = 0, hi = a.picks;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ids[mid] < col) lo = mid + 1;
+        else hi = mid;
+    }
+    r.pick = lo;
+    r.next = lo < a.picks ? ids[lo] : INT32_MAX;
+}
+// The listed columns among 32 from col0 on: PUT sets x there to what pick_x holds, otherwise pick_x gets x.
+template <bool PUT>
+__device__ __forceinline__ void pick_slice(const LmheadArgs& a, RowState& r, int col0, float (&x)[32]) {
+    while (r.next < col0 + 32) {
+        const int64_t at = r.grow * a.picks + r.pick;
+        if (r.next >= col0) {                          // (a thread skips what lies in the other column half)
+            float v = PUT ? a.pick_x[at] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col0 + i == r.next) {
+                    if (PUT) x[i] = v;
+                    else v = x[i];
+                }
+            if (!PUT) a.pick_x[at] = v;
+        }
+        ++r.pick;
+        r.next = r.pick < a.picks ? a.pick_ids[at + 1] : INT32_MAX;
+    }
 }
 
 // 32 consecutive logits of the row, from column col0 on.  `store`: the row's scratch is wanted (kFwdKeep, recompute).
@@ -241,7 +278,18 @@ template <int MODE>
 __device__ __forceinline__ void row_slice(const LmheadArgs& a, RowState& r, int col0, float (&x)[32], bool store) {
     constexpr bool KEEP = keep_mode(MODE);
     uint32_t pk[16];
-    if (base_mode(MODE) == kBwdP) {
+    if (pick_mode(MODE)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] *= a.x_scale;
+    }
+    if (base_mode(MODE) == kBwdP && pick_mode(MODE)) {
+        if (!store || col0 >= a.ncols) return;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = r.valid ? r.mul * ex2(fmaf(x[i], kLog2e, -r.off2)) : 0.f;
+        pick_slice<true>(a, r, col0, x);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) pk[i >> 1] = pack_bf16(x[i], x[i + 1]);
+    } else if (base_mode(MODE) == kBwdP) {
         if (!store || col0 >= a.ncols) return;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
@@ -252,7 +300,8 @@ __device__ __forceinline__ void row_slice(const LmheadArgs& a, RowState& r, int 
             pk[i >> 1] = pack_bf16(r.valid ? r.mul * p0 : 0.f, r.valid ? r.mul * p1 : 0.f);
         }
     } else {
-        if (r.y >= col0 && r.y < col0 + 32) {
+        if (pick_mode(MODE)) pick_slice<false>(a, r, col0, x);
+        else if (r.y >= col0 && r.y < col0 + 32) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (col0 + i == r.y) r.zy = x[i];

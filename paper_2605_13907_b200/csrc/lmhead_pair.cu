@@ -47,6 +47,18 @@ __device__ __forceinline__ void store_dw(const LmheadArgs& a, int64_t row, int c
     }
 }
 
+__device__ __forceinline__ void store_dw_half(const LmheadArgs& a, int64_t row, int col0, const uint32_t (&v)[32]) {
+    uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dW_half) + row * a.lddw + col0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (col0 + j * 8 >= a.ncols) continue;
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = pack_bf16(__uint_as_float(v[8 * j + 2 * k]), __uint_as_float(v[8 * j + 2 * k + 1]));
+        dst[j] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
 template <int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 lmhead_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -66,7 +78,7 @@ lmhead_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     constexpr int BASE = base_mode(MODE);
     constexpr bool B_MN = b_mn_major(MODE);
     constexpr bool FP8 = MODE == kFwdFp8T;
-    constexpr bool DW = MODE == kBwdDw;
+    constexpr bool DW = BASE == kBwdDw;
     constexpr int UNIT = DW ? kBwdDw : kFwdFp8;  // units of two row tiles, for decode_unit / unit_active
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int num_units = count_units<UNIT>(a);
@@ -260,6 +272,7 @@ lmhead_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 2 && !DW; ++i) {
                 r[i] = begin_row<MODE>(a, lrow0 + i * kBM, flags);
+                if (pick_mode(MODE)) pick_start(a, r[i], w.t0 * kBN + half * 128);
                 // a gated pass leaves the rows of a tile alone that was not marked, even beside one that was
                 const bool mine = !gated || (a.tile_active[a.row0 / kBM + 2 * static_cast<int64_t>(w.rt) + i * (r[i].in ? 1 : 0)] != 0);
                 store[i] = r[i].in && (BASE == kBwdP ? mine : r[i].lrow < a.keep_rows);
@@ -298,7 +311,8 @@ lmhead_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                         if (row < a.rows) {
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
-                                store_dw(a, row, col_base + c * 32, v[c]);
+                                if (MODE == kBwdDwHalf) store_dw_half(a, row, col_base + c * 32, v[c]);
+                                else store_dw(a, row, col_base + c * 32, v[c]);
                         }
                         continue;
                     }
@@ -358,13 +372,22 @@ cudaError_t launch_lmhead_pair(int mode, const CUtensorMap& tmA, const CUtensorM
         case kBwdPDv:    return launch<kBwdPDv>(tmA, tmB, tmB2, args, num_ctas, stream);
         case kFwdFp8T:   return launch<kFwdFp8T>(tmA, tmB, tmB2, args, num_ctas, stream);
         case kBwdDw:     return launch<kBwdDw>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPick: return launch<kFwdPick>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPickDv: return launch<kFwdPickDv>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPickKeep: return launch<kFwdPickKeep>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPickKeepDv: return launch<kFwdPickKeepDv>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kBwdPPick: return launch<kBwdPPick>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kBwdPPickDv: return launch<kBwdPPickDv>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kBwdDwHalf: return launch<kBwdDwHalf>(tmA, tmB, tmB2, args, num_ctas, stream);
     }
     return cudaErrorInvalidValue;
 }
 
 cudaError_t lmhead_pair_prepare() {
     const cudaError_t all[] = {prepare<kFwdBf16>(), prepare<kFwdBf16Dv>(), prepare<kFwdKeep>(), prepare<kFwdKeepDv>(),
-                               prepare<kBwdP>(),    prepare<kBwdPDv>(),    prepare<kFwdFp8T>(),   prepare<kBwdDw>()};
+                               prepare<kBwdP>(),    prepare<kBwdPDv>(),    prepare<kFwdFp8T>(),   prepare<kBwdDw>(),
+                               prepare<kFwdPick>(), prepare<kFwdPickDv>(), prepare<kFwdPickKeep>(), prepare<kFwdPickKeepDv>(),
+                               prepare<kBwdPPick>(), prepare<kBwdPPickDv>(), prepare<kBwdDwHalf>()};
     for (const cudaError_t e : all)
         if (e != cudaSuccess) return e;
     return cudaSuccess;
