@@ -5,20 +5,25 @@
 // entry that is kept, as a 64-bit number (order key of the value above, index below) whose natural order is the row's order.
 //  top-k : the k-th number.                       top-p : the first number at which the mass reaches p times the total.
 //  min-p : e >= m, a threshold on the value.       The token: the first index at which the kept mass exceeds u times its total.
-// with e = exp((x - max) / T).  Nothing is sorted but the few entries around a cut.
+// with e = exp((x - max) / T).
 //
-// A row belongs to a cluster of CTAs (one to eight); each keeps its slice of the row in shared memory, so that HBM is read once.
-//  1. slice to shared memory, maximum;   2. histogram of the distance below the maximum (2,048 bins of 1/64 of a unit of
-//  log-probability; a bin is a range of the order), and the fp32 sum of exponentials;   3. the bin of the cut: by counts for
-//  top-k; for top-p the counts give bounds on the mass above every bin, and only the bins between the bounds get their masses
-//  added up;   4. the entries of that bin go to one CTA, which sorts them and finds the cut; a bin of more than 2,048 entries (many
-//  equal values, a degenerate temperature) is first divided by the number itself, 2,048 ways at a time.
-// A top-k of at most 1,024 takes all entries down to its bin into that list, and the rest happens there.
+// A row belongs to a cluster of one to eight CTAs, a slice each.  What bounds the kernels is one read of the logits for many rows,
+// and the chain of block and cluster barriers for few; so every case reads the row as few times as it can.
+//  * The K largest (top_logits, top-k up to 1,024): one pass.  The first tile of a slice gives a threshold (the K-th largest of the
+//    maxima of 256 to 1,024 groups of entries: K entries reach it), later entries above it join a list in shared memory, and the list is cut
+//    back to its K largest when it fills up, which raises the threshold.  Lists of all slices are sorted together at the end.
+//  * No filter: one pass of fp64 sums per warp, then the one warp's range that holds the token is read again.
+//  * Everything else (top-p or min-p over the whole row, longer top-k, lists that overflow, values out of fp32's range): passes over
+//    data that is mostly still in L1 or L2.  Maximum; histogram of the distance below it (2,048 bins of 1/64 of a unit of log-probability;
+//    a bin is a range of the order); for top-p the counts give bounds on the mass above every bin, and one pass of fp64
+//    exponentials adds up the mass above the bounds per warp and that of the bins between them per bin.  The entries of the bin
+//    with the cut go to one CTA, which sorts them; a bin of more entries than its list holds is first divided by the number
+//    itself, 2,048 ways at a time.
 //
 // Precision: which token is drawn and how many are kept are decided by comparing sums over the vocabulary with borders; fp32
-// sums (1e-7 relative) would decide one row in a hundred differently.  Masses are 64-bit integers, exponentials in fp64 rounded
-// to multiples of 2^-44 (sums of 2^18 terms stay below 2^63): exact to add in any order, so the result does not depend on the
-// order of atomics.
+// sums (1e-7 relative) would decide one row in a hundred differently.  Exponentials and sums that decide are fp64, summed in an
+// order that the sizes fix.  Sums by atomics (masses of bins) are 64-bit integers, exponentials rounded to multiples of 2^-44: exact to
+// add in any order, so no result depends on the order of atomics.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -39,40 +44,47 @@ namespace {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight, in the pass for the largest entries
+constexpr int kBatch = 2;                // and in the others, beside as many that are worked on
 constexpr int kBins = 2048;
 constexpr int kBinsPerThread = kBins / kSelThreads;
-constexpr int kListCap = 2048;           // entries of the list that one CTA sorts
+constexpr int kListCap = 4096;           // entries of a list
+constexpr int kListPrune = 2048;         // a list is cut back beyond this
+constexpr int kRankSort = 256;           // entries up to which a list is sorted by counting
 constexpr int kMaxCluster = 8;
-constexpr int kSliceBytes = 160 * 1024;  // most of a row that a CTA holds
 constexpr float kBinsPerNat = 64.f;
 constexpr int kIndexBits = 20;
 constexpr double kMassOne = 17592186044416.0;   // 2^44
+constexpr int kTableCopies = 16;         // of the table of powers of two
 
 typedef unsigned long long u64;
 
 struct Published {                       // what a CTA tells the others of its cluster
-    float max;
+    float top;
     int bad;
-    u64 mass[3];
+    double sum[2];
     u64 lo, hi;
-    double full;
     int count;
 };
 
 struct alignas(16) SelShared {
     uint32_t hist[kBins];                // of this CTA's slice
-    uint32_t tot[kBins];                 // of the row
-    u64 mass[kBins];
+    uint32_t tot[kBins];                 // of the row (more than one CTA)
     union {
-        u64 mass_tot[kBins];
+        struct {
+            u64 mass[kBins];
+            u64 mass_tot[kBins];
+        };
         u64 list[kListCap];
     };
+    double exp2_table[64 * kTableCopies];   // 2^(j / 64)
+    double warp_kept[kSelWarps];         // kept mass of every warp's range
     Published pub;
-    u64 warp_u64[kSelWarps];
-    u64 warp_u64b[kSelWarps];
-    double warp_f64[kSelWarps];
+    double warp_f64[2][kSelWarps];
+    u64 warp_u64[2][kSelWarps];
     int warp_int[kSelWarps];
-    u64 found[4];
+    double found_mass;
+    int found[4];
     int list_n;
 };
 
@@ -81,7 +93,6 @@ struct SelectArgs {
     int64_t ld;
     int V;
     int cluster;
-    int slice;               // elements per CTA, a multiple of 64
     const uint8_t* mask;
     uint32_t* status;
     // sampling
@@ -102,10 +113,40 @@ struct SelectArgs {
 // 0 (the largest entry) or at least AIS_MIN_TEMPERATURE; not NaN, not infinite.
 __host__ __device__ inline bool usable_temperature(float t) { return t == 0.f || (t >= AIS_MIN_TEMPERATURE && t < INFINITY); }
 
-template <typename T> __device__ __forceinline__ float to_f32(T v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static constexpr int kEach = 4;
+    static constexpr uint32_t kNegInf = 0xff800000u;
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+    }
+};
+template <> struct Elem<__nv_bfloat16> {
+    static constexpr int kEach = 8;
+    static constexpr uint32_t kNegInf = 0xff80ff80u;
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+    }
+};
+template <> struct Elem<__half> {
+    static constexpr int kEach = 8;
+    static constexpr uint32_t kNegInf = 0xfc00fc00u;
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+            x[2 * j] = f.x;
+            x[2 * j + 1] = f.y;
+        }
+    }
+};
 
 // The order of a row as one number: larger values first, -0 and 0 alike, then the smaller index.
 __device__ __forceinline__ u64 order_of(float x, int index) {
@@ -121,24 +162,14 @@ __device__ __forceinline__ int index_of(u64 o) { return static_cast<int>(o & ((1
 // the last number of a finite entry
 __device__ __forceinline__ u64 last_finite() { return order_of(-INFINITY, 0) - 1; }
 
-struct Scale {
-    float top;
-    double inv_t;
-    float bins;             // bins per unit of x
-    float log2_scale;       // log2(e) / T
-    __device__ __forceinline__ int bin(float x) const {
-        const float y = (top - x) * bins;
-        return y < static_cast<float>(kBins - 1) ? static_cast<int>(y) : kBins - 1;
-    }
-    __device__ __forceinline__ double logw(float x) const { return (static_cast<double>(x) - static_cast<double>(top)) * inv_t; }
-    __device__ __forceinline__ u64 mass(float x) const { return __double2ull_rn(exp(logw(x)) * kMassOne); }
-};
-
-__device__ __forceinline__ u64 warp_sum(u64 v) {
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ double warp_sum(double v) {
+
+template <typename N>
+__device__ __forceinline__ N warp_sum(N v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
@@ -169,30 +200,161 @@ __device__ __forceinline__ N block_scan(N v, N* scratch, N& total) {
     return before + inc - v;
 }
 
-// What a kernel holds of one row.
+// Ascending, n2 a power of two.
+template <typename N>
+__device__ void block_sort(N* v, int n2) {
+    for (int size = 2; size <= n2; size <<= 1)
+        for (int stride = size >> 1; stride > 0; stride >>= 1) {
+            for (int t = threadIdx.x; t < n2 / 2; t += kSelThreads) {
+                const int i = 2 * t - (t & (stride - 1)), j = i + stride;
+                const N a = v[i], b = v[j];
+                if ((a > b) == ((i & size) == 0)) {
+                    v[i] = b;
+                    v[j] = a;
+                }
+            }
+            __syncthreads();
+        }
+}
+__device__ __forceinline__ int pow2_from(int n) {
+    int n2 = 2;
+    while (n2 < n) n2 <<= 1;
+    return n2;
+}
+
+// e^((x - ref) / T) in fp64 for a fixed T and ref: 2^(k / 64) from a table times a polynomial in the rest, at most ln 2 / 128 (Taylor
+// series to the fourth power: 4e-14 relative).  Ten fp64 instructions and a look-up; exp() takes more than twice that.  The table is
+// there sixteen times, entry j of copy c at 16 j + c, so that the 16 lanes of a half-warp read 16 different pairs of banks (one
+// copy: 5 instead of 2 cycles per look-up).
+struct Weight {
+    double c64, ref;          // 64 log2(e) / T
+    float floor;              // entries below this get no weight (-inf among them); their weight is below 2^-1000
+    __device__ __forceinline__ void set(double inv_t, double ref_) {
+        c64 = 92.332482616893656877 * inv_t;
+        ref = ref_;
+        floor = __double2float_ru(fmax(ref - 64000.0 / c64, -3.4028234663852886e38));     // (no more than ref)
+    }
+    // x >= floor.  (The difference first: with one fused multiply-add for both, ref itself would weigh 1 only to within the rounding of
+    // ref / T, and logits of 1e30 anything.)
+    __device__ __forceinline__ double of(const double* table, float x) const {
+        constexpr double kMagic = 6755399441055744.0;            // 1.5 x 2^52
+        constexpr double a1 = 0.010830424696249145, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;   // ln(2) / 64
+        const double y = (static_cast<double>(x) - ref) * c64;
+        const double t = y + kMagic;
+        const int k = __double2loint(t);
+        const double f = y - (t - kMagic);
+        const double p = f * fma(f, fma(f, fma(f, a4, a3), a2), a1);
+        const double e = table[(k & 63) * kTableCopies + (threadIdx.x & (kTableCopies - 1))];
+        const double w = fma(e, p, e);
+        return __hiloint2double(__double2hiint(w) + ((k >> 6) << 20), __double2loint(w));
+    }
+    __device__ __forceinline__ double operator()(const double* table, float x) const {
+        const double w = of(table, fmaxf(x, floor));
+        return x >= floor ? w : 0.0;
+    }
+};
+
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// What a CTA holds of one row.
 template <typename T>
 struct Row {
+    static constexpr int kEach = Elem<T>::kEach;
     SelShared& s;
-    const T* data;           // this CTA's slice in shared memory
-    int begin, n;            // where it starts in the row, its length
+    const T* x;              // the row
+    int V, head;             // its length; elements before the first 16-byte boundary
+    int whole;               // 16-byte chunks behind that
+    int c0, c1;              // this CTA's
     int C, rank;
-    Scale sc;
+    float top;               // largest value (once known)
+    float bins;              // histogram bins per unit of x
+    double inv_t;
+    Weight weight;           // about `top`
 
-    __device__ __forceinline__ float at(int i) const { return to_f32(data[i]); }
+    __device__ Row(SelShared& shared, const SelectArgs& a, int64_t row, int rank_) : s(shared), V(a.V), C(a.cluster), rank(rank_) {
+        x = static_cast<const T*>(a.x) + row * a.ld;
+        head = min(static_cast<int>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T)), V);
+        whole = (V - head) / kEach;
+        const int per = (whole + C - 1) / C;
+        c0 = min(rank * per, whole);
+        c1 = min(c0 + per, whole);
+    }
+    __device__ __forceinline__ int first_index(int c) const { return head + c * kEach; }
+    __device__ __forceinline__ uint4 chunk(int c, int end) const {            // -inf from `end` on
+        return c < end ? *reinterpret_cast<const uint4*>(x + first_index(c))
+                       : make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
+    }
+    // The entries before the first and behind the last whole chunk, fewer than kEach each, belong to the first warp of the first CTA
+    // (before its chunks) and to the last warp of the last CTA (behind its chunks).  One of them as a chunk filled up with -inf at its end;
+    // false if there is none (for this warp).
+    __device__ __forceinline__ bool edge(bool tail, float (&v)[kEach], int& i) const {
+        const int warp = threadIdx.x >> 5;
+        int n;
+        if (tail) {
+            i = first_index(whole);
+            n = rank == C - 1 && warp == kSelWarps - 1 ? V - i : 0;
+        } else {
+            i = 0;
+            n = rank == 0 && warp == 0 ? head : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) v[k] = k < n ? to_f32(x[i + k]) : -INFINITY;
+        return n > 0;
+    }
+    // A warp owns consecutive chunks of the slice.
+    __device__ __forceinline__ void range(int& from, int& to) const {
+        const int per = ((c1 - c0 + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
+        from = min(c0 + static_cast<int>(threadIdx.x >> 5) * per, c1);
+        to = min(from + per, c1);
+    }
+    // f(values, index of the first, how many are part of the row) for everything this warp owns, a thread at a time.  kBatch chunks are
+    // in flight while as many are worked on; the loop holds the code of no more (32 exponentials did not fit the instruction cache).
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        int from, to;
+        range(from, to);
+        const int lane = threadIdx.x & 31;
+        uint4 raw[kBatch], next[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) raw[j] = chunk(from + lane + 32 * j, to);
+#pragma unroll 1
+        for (int c = from + lane; c < to; c += 32 * kBatch) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) next[j] = chunk(c + 32 * (kBatch + j), to);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                float v[kEach];
+                Elem<T>::unpack(raw[j], v);
+                if (j == 0 || c + 32 * j < to) f(v, first_index(c + 32 * j), kEach);
+                raw[j] = next[j];
+            }
+        }
+        // the ends of the row: lane 0 the head, lane 1 the tail
+        if (lane < 2) {
+            float v[kEach];
+            int i;
+            if (edge(lane == 1, v, i)) f(v, i, lane == 1 ? V - i : head);
+        }
+    }
+
     __device__ void sync() const {
         if (C > 1) cg::this_cluster().sync();
         else __syncthreads();
     }
     template <typename P>
     __device__ P* remote(P* p, int r) const { return C > 1 ? cg::this_cluster().map_shared_rank(p, r) : p; }
-
-    // f(x, i) for the elements of the slice, warp by warp in order of the index: a warp owns consecutive elements
-    __device__ __forceinline__ int segment() const { return (n + kSelWarps * 32 - 1) / (kSelWarps * 32) * 32; }
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        const int seg = segment(), lane = threadIdx.x & 31, from = (threadIdx.x >> 5) * seg, to = min(from + seg, n);
-        for (int i = from + lane; i < to; i += 32) f(at(i), i);
+    __device__ __forceinline__ int bin(float v) const {
+        const float y = (top - v) * bins;
+        return y < static_cast<float>(kBins - 1) ? static_cast<int>(y) : kBins - 1;
     }
+    __device__ __forceinline__ u64 mass(float v) const { return __double2ull_rn(weight(s.exp2_table, v) * kMassOne); }
+    __device__ __forceinline__ const uint32_t* counts() const { return C > 1 ? s.tot : s.hist; }
+    __device__ __forceinline__ const u64* masses() const { return C > 1 ? s.mass_tot : s.mass; }
+
     __device__ void clear_hist(bool with_mass) const {
         for (int b = threadIdx.x; b < kBins; b += kSelThreads) {
             s.hist[b] = 0;
@@ -203,6 +365,7 @@ struct Row {
     // hist (and mass) of all slices added up in every CTA
     __device__ void merge_hist(bool with_mass) const {
         sync();
+        if (C == 1) return;
         const int share = kBins / C;
         for (int i = threadIdx.x; i < share; i += kSelThreads) {
             const int b = rank * share + i;
@@ -219,14 +382,68 @@ struct Row {
         }
         sync();
     }
+    // Two sums, a count and (with MAX) the largest value of all CTAs; `before`: sum[0] of the CTAs ahead of this one.
+    struct Totals {
+        double sum[2], before;
+        float top;
+        int count, bad;
+    };
+    template <bool MAX>
+    __device__ Totals add_up(double a, double b, int count, float top_, int bad) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        a = warp_sum(a);
+        b = warp_sum(b);
+        const int c = __reduce_add_sync(0xffffffffu, count);
+        if (MAX) {
+            for (int o = 16; o > 0; o >>= 1) top_ = fmaxf(top_, __shfl_xor_sync(0xffffffffu, top_, o));
+            bad = __reduce_or_sync(0xffffffffu, bad);
+        }
+        __syncthreads();
+        if (lane == 0) {
+            s.warp_f64[0][warp] = a;
+            s.warp_f64[1][warp] = b;
+            s.warp_int[warp] = c;
+            if (MAX) s.warp_u64[0][warp] = (static_cast<u64>(bad) << 32) | __float_as_uint(top_);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            a = b = 0.0;
+            int n = 0;
+            for (int w = 0; w < kSelWarps; ++w) {
+                a += s.warp_f64[0][w];
+                b += s.warp_f64[1][w];
+                n += s.warp_int[w];
+                if (MAX) {
+                    top_ = fmaxf(top_, __uint_as_float(static_cast<uint32_t>(s.warp_u64[0][w])));
+                    bad |= static_cast<int>(s.warp_u64[0][w] >> 32);
+                }
+            }
+            s.pub.sum[0] = a;
+            s.pub.sum[1] = b;
+            s.pub.count = n;
+            if (MAX) { s.pub.top = top_; s.pub.bad = bad; }
+        }
+        sync();
+        Totals t = {{0.0, 0.0}, 0.0, -INFINITY, 0, 0};
+        for (int r = 0; r < C; ++r) {
+            const Published* p = remote(&s.pub, r);
+            if (r == rank) t.before = t.sum[0];
+            t.sum[0] += p->sum[0];
+            t.sum[1] += p->sum[1];
+            t.count += p->count;
+            if (MAX) { t.top = fmaxf(t.top, p->top); t.bad |= p->bad; }
+        }
+        sync();
+        return t;
+    }
     // The bin in which the count reaches k (k >= 1, no more than the total): s.found = {bin, entries before it, entries in it}.
-    __device__ void find_count(u64 k) const {
+    __device__ void find_count(int k) const {
         const int b0 = threadIdx.x * kBinsPerThread;
         int c[kBinsPerThread], sum = 0, total;
-        for (int j = 0; j < kBinsPerThread; ++j) sum += c[j] = static_cast<int>(s.tot[b0 + j]);
+        for (int j = 0; j < kBinsPerThread; ++j) sum += c[j] = static_cast<int>(counts()[b0 + j]);
         int before = block_scan(sum, s.warp_int, total);
         for (int j = 0; j < kBinsPerThread; ++j) {
-            if (static_cast<u64>(before) < k && static_cast<u64>(before + c[j]) >= k) {
+            if (before < k && before + c[j] >= k) {
                 s.found[0] = b0 + j;
                 s.found[1] = before;
                 s.found[2] = c[j];
@@ -235,79 +452,169 @@ struct Row {
         }
         __syncthreads();
     }
-    // The bin in which mass0 plus the masses reach p total: s.found = {bin, mass before it, entries in it}; the last bin with an
-    // entry where rounding leaves none.
-    __device__ void find_mass(u64 mass0, double target) const {
+    // The bin in which mass0 plus the masses reach the target: s.found = {bin, -, entries in it, whether there is one}, s.found_mass the
+    // mass before it.
+    __device__ void find_mass(double mass0, double target) const {
         if (threadIdx.x == 0) s.found[3] = 0;
         const int b0 = threadIdx.x * kBinsPerThread;
         u64 m[kBinsPerThread], sum = 0, total;
-        for (int j = 0; j < kBinsPerThread; ++j) sum += m[j] = s.mass_tot[b0 + j];
-        u64 before = mass0 + block_scan(sum, s.warp_u64, total);
+        for (int j = 0; j < kBinsPerThread; ++j) sum += m[j] = masses()[b0 + j];
+        u64 before = block_scan(sum, s.warp_u64[0], total);
         for (int j = 0; j < kBinsPerThread; ++j) {
-            if (static_cast<double>(before) < target && static_cast<double>(before + m[j]) >= target) {
+            const double lo = mass0 + static_cast<double>(before), hi = mass0 + static_cast<double>(before + m[j]);
+            if (m[j] != 0 && lo < target && hi >= target) {
                 s.found[0] = b0 + j;
-                s.found[1] = before;
-                s.found[2] = s.tot[b0 + j];
+                s.found[2] = counts()[b0 + j];
                 s.found[3] = 1;
+                s.found_mass = lo;
             }
             before += m[j];
         }
         __syncthreads();
     }
-    // Entries for which keep(x, order) go to the list of rank 0, sorted there.  Every CTA returns after the list is complete;
-    // only rank 0 has it.
+    // Entries that keep(value, order) takes go to the list of rank 0, sorted there; only rank 0 has it (and its length, at most kListCap).
     template <typename F>
     __device__ int gather_sorted(F keep) const {
-        sync();                                    // the list shares its place with mass_tot
+        sync();                                    // the list shares its place with the masses
         if (threadIdx.x == 0) s.list_n = 0;
         sync();
         int* counter = remote(&s.list_n, 0);
         u64* list = remote(s.list, 0);
-        each([&](float x, int i) {
-            const u64 o = order_of(x, begin + i);
-            if (keep(x, o)) {
-                const int at = atomicAdd(counter, 1);
-                if (at < kListCap) list[at] = o;
+        each([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const u64 o = order_of(v[k], i + k);
+                if (keep(v[k], o)) {
+                    const int at = atomicAdd(counter, 1);
+                    if (at < kListCap) list[at] = o;
+                }
             }
         });
         sync();
         if (rank != 0) return 0;
-        const int n_list = min(s.list_n, kListCap);
-        int n2 = 2;
-        while (n2 < n_list) n2 <<= 1;
-        for (int i = n_list + threadIdx.x; i < n2; i += kSelThreads) s.list[i] = ~0ull;
-        __syncthreads();
-        for (int size = 2; size <= n2; size <<= 1)
-            for (int stride = size >> 1; stride > 0; stride >>= 1) {
-                for (int t = threadIdx.x; t < n2 / 2; t += kSelThreads) {
-                    const int i = 2 * t - (t & (stride - 1)), j = i + stride;
-                    const u64 a = s.list[i], b = s.list[j];
-                    if ((a > b) == ((i & size) == 0)) {
-                        s.list[i] = b;
-                        s.list[j] = a;
-                    }
-                }
-                __syncthreads();
-            }
-        return n_list;
+        return sort_list(min(s.list_n, kListCap));
     }
-    // Smallest and largest number of the entries that pick(x, order) takes.
+    __device__ int sort_list(int n) const {
+        const int n2 = pow2_from(n);
+        if (n <= kRankSort) {                                     // every entry counts those before it
+            const u64 o = threadIdx.x < n ? s.list[threadIdx.x] : 0;
+            int at = 0;
+            for (int i = 0; threadIdx.x < n && i < n; ++i) at += s.list[i] < o;
+            __syncthreads();
+            if (threadIdx.x < n) s.list[at] = o;
+            __syncthreads();
+            return n;
+        }
+        for (int i = n + threadIdx.x; i < n2; i += kSelThreads) s.list[i] = ~0ull;
+        __syncthreads();
+        block_sort(s.list, n2);
+        return n;
+    }
+    // A value that at least K of the n values val(i) reach, no more than K / 4 + 8 others if no value is given too often; -inf where
+    // fewer than K are finite.  Histograms of 512 bins, each over the bin of the K-th value of the one before.
+    template <typename F>
+    __device__ float bound(F val, int n, int K, float* largest = nullptr) const {
+        float lo = INFINITY, hi = -INFINITY;
+        auto extend = [&](float& l, float& h) {                   // over the block
+            for (int o = 16; o > 0; o >>= 1) {
+                l = fminf(l, __shfl_xor_sync(0xffffffffu, l, o));
+                h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, o));
+            }
+            float2* part = reinterpret_cast<float2*>(s.warp_u64[1]);
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(l, h);
+            __syncthreads();
+            for (int w = 0; w < kSelWarps; ++w) {
+                l = fminf(l, part[w].x);
+                h = fmaxf(h, part[w].y);
+            }
+        };
+        for (int i = threadIdx.x; i < n; i += kSelThreads) {
+            const float v = val(i);
+            if (v > -INFINITY) { lo = fminf(lo, v); hi = fmaxf(hi, v); }
+        }
+        extend(lo, hi);
+        if (largest) *largest = hi;
+        int ahead = 0;
+        for (int level = 0; level < 5; ++level) {
+            const float scale = hi > lo ? fminf(511.9f / (hi - lo), 1e38f) : 0.f;
+            static_assert(kSelThreads == 512, "a thread per bin");
+            s.hist[threadIdx.x] = 0;
+            if (threadIdx.x == 0) s.found[0] = -1;
+            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += kSelThreads) {
+                const float v = val(i);
+                if (v >= lo && v <= hi) atomicAdd(&s.hist[min(static_cast<int>((hi - v) * scale), 511)], 1u);
+            }
+            __syncthreads();
+            const int c = static_cast<int>(s.hist[threadIdx.x]);
+            int total;
+            const int before = ahead + block_scan(c, s.warp_int, total);
+            if (before < K && before + c >= K) {
+                s.found[0] = threadIdx.x;
+                s.found[1] = before;
+                s.found[2] = c;
+            }
+            __syncthreads();
+            const int b = s.found[0], reach = s.found[1] + s.found[2];
+            if (b < 0) return -INFINITY;
+            ahead = s.found[1];
+            float l = INFINITY, h = -INFINITY;
+            for (int i = threadIdx.x; i < n; i += kSelThreads) {
+                const float v = val(i);
+                if (v >= lo && v <= hi && min(static_cast<int>((hi - v) * scale), 511) == b) { l = fminf(l, v); h = fmaxf(h, v); }
+            }
+            extend(l, h);
+            lo = l;
+            hi = h;
+            if (reach <= K + K / 4 + 8 || lo == hi) break;
+        }
+        return lo;
+    }
+    // The list without the entries below `thr`.
+    __device__ void drop_below(float thr, int n) const {
+        constexpr int kMine = kListCap / kSelThreads;
+        u64 o[kMine];
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) o[j] = threadIdx.x + j * kSelThreads < n ? s.list[threadIdx.x + j * kSelThreads] : ~0ull;
+        __syncthreads();
+        if (threadIdx.x == 0) s.list_n = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+            if (o[j] != ~0ull && value_of(o[j]) >= thr) s.list[atomicAdd(&s.list_n, 1)] = o[j];
+        __syncthreads();
+    }
+    // The K largest of the first n entries of the list, sorted; returns their number.
+    __device__ int sort_top(int n, int K) const {
+        if (n > kRankSort && n > K + K / 4 + 8) {
+            const float thr = bound([&](int i) { return value_of(s.list[i]); }, n, K);
+            drop_below(thr, n);
+            n = s.list_n;
+            __syncthreads();
+        }
+        return min(sort_list(n), K);
+    }
+    // Smallest and largest number of the entries that pick(value, order) takes.
     template <typename F>
     __device__ void range_of(F pick, u64& lo, u64& hi) const {
         u64 a = ~0ull, b = 0;
-        each([&](float x, int i) {
-            const u64 o = order_of(x, begin + i);
-            if (pick(x, o)) { a = min(a, o); b = max(b, o); }
+        each([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const u64 o = order_of(v[k], i + k);
+                if (pick(v[k], o)) { a = min(a, o); b = max(b, o); }
+            }
         });
         for (int o = 16; o > 0; o >>= 1) {
             a = min(a, __shfl_xor_sync(0xffffffffu, a, o));
             b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
         }
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) { s.warp_u64[threadIdx.x >> 5] = a; s.warp_u64b[threadIdx.x >> 5] = b; }
+        if ((threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = a; s.warp_u64[1][threadIdx.x >> 5] = b; }
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 0; w < kSelWarps; ++w) { a = min(a, s.warp_u64[w]); b = max(b, s.warp_u64b[w]); }
+            for (int w = 0; w < kSelWarps; ++w) { a = min(a, s.warp_u64[0][w]); b = max(b, s.warp_u64[1][w]); }
             s.pub.lo = a;
             s.pub.hi = b;
         }
@@ -320,55 +627,56 @@ struct Row {
         }
         sync();
     }
-    // The cut inside a group of `count` entries, those that pick(x, order) takes: by count, the entry number `want` (from 1) of the
+    // The cut inside a group of `count` entries, those that pick(value, order) takes: by count, the entry number `want` (from 1) of the
     // group; by mass, the first at which mass0 plus the masses reach `target`.
     template <bool MASS, typename F>
-    __device__ u64 cut_in_group(F pick, int count, u64 want, u64 mass0, double target) const {
-        if (count > kListCap) {
-            u64 lo, hi;
-            range_of(pick, lo, hi);
-            while (count > kListCap && lo < hi) {
-                const int bits = 64 - __clzll(hi - lo);
-                const int shift = bits > 11 ? bits - 11 : 0;
-                clear_hist(MASS);
-                each([&](float x, int i) {
-                    const u64 o = order_of(x, begin + i);
-                    if (o < lo || o > hi) return;
+    __device__ u64 cut_in_group(F pick, int count, int want, double mass0, double target) const {
+        if (count <= kListCap) return cut_in_list<MASS>(pick, want, mass0, target);
+        u64 lo, hi;
+        range_of(pick, lo, hi);
+        while (count > kListCap) {                               // (a single number is one entry)
+            const int bits = 64 - __clzll(hi - lo);
+            const int shift = bits > 11 ? bits - 11 : 0;
+            clear_hist(MASS);
+            each([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) {
+                    const u64 o = order_of(v[k], i + k);
+                    if (o < lo || o > hi) continue;
                     const int b = static_cast<int>((o - lo) >> shift);
                     atomicAdd(&s.hist[b], 1u);
-                    if (MASS) atomicAdd(&s.mass[b], sc.mass(x));
-                });
-                merge_hist(MASS);
-                if (MASS) {
-                    find_mass(mass0, target);
-                    if (s.found[3] == 0) return hi;                  // rounding: the whole group
-                    mass0 = s.found[1];
-                } else {
-                    find_count(want);
-                    want -= s.found[1];
+                    if (MASS) atomicAdd(&s.mass[b], mass(v[k]));
                 }
-                count = static_cast<int>(s.found[2]);
-                lo += s.found[0] << shift;
-                hi = min(hi, lo + ((1ull << shift) - 1));
+            });
+            merge_hist(MASS);
+            if (MASS) {
+                find_mass(mass0, target);
+                if (s.found[3] == 0) return hi;                  // rounding: the whole group
+                mass0 = s.found_mass;
+            } else {
+                find_count(want);
+                want -= s.found[1];
             }
-            if (lo == hi) return lo;
-            return cut_in_list<MASS>([=](float, u64 o) { return o >= lo && o <= hi; }, want, mass0, target);
+            count = s.found[2];
+            lo += static_cast<u64>(s.found[0]) << shift;
+            hi = min(hi, lo + ((1ull << shift) - 1));
+            __syncthreads();
         }
-        return cut_in_list<MASS>(pick, want, mass0, target);
+        return cut_in_list<MASS>([=](float, u64 o) { return o >= lo && o <= hi; }, want, mass0, target);
     }
     template <bool MASS, typename F>
-    __device__ u64 cut_in_list(F pick, u64 want, u64 mass0, double target) const {
+    __device__ u64 cut_in_list(F pick, int want, double mass0, double target) const {
         const int n_list = gather_sorted(pick);
         if (rank == 0) {
             if (MASS) {
-                constexpr int kEach = kListCap / kSelThreads;
-                u64 m[kEach], sum = 0, total;
-                const int i0 = threadIdx.x * kEach;
-                for (int j = 0; j < kEach; ++j) sum += m[j] = i0 + j < n_list ? sc.mass(value_of(s.list[i0 + j])) : 0;
+                constexpr int kMine = kListCap / kSelThreads;
+                u64 m[kMine], sum = 0, total;
+                const int i0 = threadIdx.x * kMine;
+                for (int j = 0; j < kMine; ++j) sum += m[j] = i0 + j < n_list ? mass(value_of(s.list[i0 + j])) : 0;
                 if (threadIdx.x == 0) s.pub.lo = s.list[n_list - 1];
-                u64 before = mass0 + block_scan(sum, s.warp_u64, total);
-                for (int j = 0; j < kEach; ++j) {
-                    if (i0 + j < n_list && static_cast<double>(before) < target && static_cast<double>(before + m[j]) >= target)
+                u64 before = block_scan(sum, s.warp_u64[0], total);
+                for (int j = 0; j < kMine; ++j) {
+                    if (i0 + j < n_list && mass0 + static_cast<double>(before) < target && mass0 + static_cast<double>(before + m[j]) >= target)
                         s.pub.lo = s.list[i0 + j];
                     before += m[j];
                 }
@@ -381,150 +689,224 @@ struct Row {
         sync();
         return cut;
     }
-    // mass[0..2], count and full of all CTAs; `before` gets the mass[0] of the CTAs ahead of this one
-    __device__ void add_up(const u64 (&mine)[3], int count, double full, u64 (&sum)[3], u64& before, int& n_sum, double& f_sum) const {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        u64 m[3];
-        for (int j = 0; j < 3; ++j) m[j] = warp_sum(mine[j]);
-        const int c = __reduce_add_sync(0xffffffffu, count);
-        const double f = warp_sum(full);
-        __syncthreads();
-        if (lane == 0) {
-            s.warp_u64[warp] = m[0];
-            s.warp_u64b[warp] = m[1];
-            s.warp_f64[warp] = f;
-            s.warp_int[warp] = c;
+
+    __device__ void set_scale(float top_, double inv_t_) {
+        top = top_;
+        inv_t = inv_t_;
+        bins = static_cast<float>(kBinsPerNat * inv_t_);
+        weight.set(inv_t, static_cast<double>(top_));
+    }
+    // The row's maximum, number of finite entries and whether it holds a NaN or +inf.
+    __device__ Totals look() const {
+        float m = -INFINITY, least = INFINITY;
+        each([&](const float (&v)[kEach], int, int n) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                m = max_nan(m, v[k]);
+                least = fminf(least, k < n ? v[k] : INFINITY);
+            }
+        });
+        return extremes(0.0, m, least);
+    }
+    // Totals of a pass that has seen this thread's maximum (NaN if there was one) and minimum.  Entries of -inf are counted only where
+    // there are any.
+    __device__ Totals extremes(double sum, float m, float least) const {
+        Totals t = add_up<true>(sum, 0.0, 0, isnan(m) ? -INFINITY : m, (m < INFINITY ? 0 : 1) | (least == -INFINITY ? 2 : 0));
+        if ((t.bad & 2) != 0) {
+            int finite = 0;
+            each([&](const float (&v)[kEach], int, int) {
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) finite += v[k] > -INFINITY;
+            });
+            t.count = add_up<false>(0.0, 0.0, finite, 0.f, 0).count;
+        } else {
+            t.count = V;
         }
+        t.bad &= 1;
+        return t;
+    }
+    // Histogram of the row, merged; returns the fp32 sum of its exponentials about `top` (this thread's part).
+    __device__ double histogram() const {
+        const float c = static_cast<float>(1.4426950408889634 * inv_t);
+        clear_hist(false);
+        double full = 0.0;
+        each([&](const float (&v)[kEach], int, int) {
+            float f = 0.f;
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                if (v[k] > -INFINITY) atomicAdd(&s.hist[bin(v[k])], 1u);
+                f += ex2_approx((v[k] - top) * c);
+            }
+            full += static_cast<double>(f);
+        });
+        merge_hist(false);
+        return full;
+    }
+
+    // The K largest entries by one pass: rank 0 gets them sorted in s.list and returns their number, and the fp32 sum of exponentials
+    // about `ref` in `full` (all threads of all CTAs).  -1: the list overflowed, or the sum says that the row needs a closer look.
+    __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
+        constexpr int kTile = kSelThreads * kDeep;
+        const float c = static_cast<float>(1.4426950408889634 * inv_t_);
+        const int n = c1 - c0;
+        float* group_max = reinterpret_cast<float*>(s.tot);       // 1,024 group maxima at most
+        if (threadIdx.x == 0) s.list_n = 0;
         __syncthreads();
-        if (threadIdx.x == 0) {
-            u64 a = 0, b = 0;
-            double t = 0.0;
-            int k = 0;
-            for (int w = 0; w < kSelWarps; ++w) { a += s.warp_u64[w]; b += s.warp_u64b[w]; t += s.warp_f64[w]; k += s.warp_int[w]; }
-            s.pub.mass[0] = a;
-            s.pub.mass[1] = b;
-            s.pub.full = t;
-            s.pub.count = k;
+        uint4 raw[kDeep];
+        float thr = -INFINITY;
+        ref = 0.f;
+        full = 0.0;
+        bool overflow = false;
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) raw[j] = chunk(c0 + j * kSelThreads + threadIdx.x, c1);
+        if (n > 0) {
+            // groups: the entries of a thread's first and of its last loads, of a thread, or of two threads
+            float half[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < kDeep; ++j) {
+                float v[kEach];
+                Elem<T>::unpack(raw[j], v);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) half[j / (kDeep / 2)] = fmaxf(half[j / (kDeep / 2)], v[k]);
+            }
+            float both = fmaxf(half[0], half[1]);
+            int groups;
+            if (K > kSelThreads / 2) {
+                groups = 2 * kSelThreads;
+                group_max[2 * threadIdx.x] = half[0];
+                group_max[2 * threadIdx.x + 1] = half[1];
+            } else if (K > kSelThreads / 8) {
+                groups = kSelThreads;
+                group_max[threadIdx.x] = both;
+            } else {
+                groups = kSelThreads / 2;
+                both = fmaxf(both, __shfl_xor_sync(0xffffffffu, both, 1));
+                if ((threadIdx.x & 1) == 0) group_max[threadIdx.x / 2] = both;
+            }
+            __syncthreads();
+            thr = bound([&](int i) { return group_max[i]; }, groups, K, &ref);
+            if (!(fabsf(ref) < INFINITY)) ref = 0.f;
         }
+        auto push = [&](const float (&v)[kEach], int i, float above) {
+            int at = 0;
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (v[k] > above) {
+                    at = atomicAdd(&s.list_n, 1);
+                    if (at < kListCap) s.list[at] = order_of(v[k], i + k);
+                }
+            return at;
+        };
+        auto ends = [&](bool tail, float above) {                 // the entries outside the whole chunks
+            float v[kEach], f = 0.f;
+            int i;
+            if ((threadIdx.x & 31) != 0 || !edge(tail, v, i)) return;
+            push(v, i, above);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) f += ex2_approx((v[k] - ref) * c);
+            full += static_cast<double>(f);
+        };
+        ends(false, thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY);
+        int tile = 0, limit = max(512, 4 * K);
+#pragma unroll 1
+        for (int t0 = 0; t0 < n; t0 += kTile, ++tile) {
+            int pushed = 0;
+            float f = 0.f;
+            // (>= in the first tile, whose entries gave the bound; later ones of the same value come after K entries in the order)
+            const float above = tile == 0 ? nextafterf(thr, -INFINITY) : thr;
+#pragma unroll 1
+            for (int j = 0; j < kDeep; ++j) {
+                float v[kEach];
+                Elem<T>::unpack(raw[0], v);
+#pragma unroll
+                for (int i = 0; i + 1 < kDeep; ++i) raw[i] = raw[i + 1];
+                raw[kDeep - 1] = chunk(c0 + t0 + (kDeep + j) * kSelThreads + threadIdx.x, c1);
+                float m = v[0];
+#pragma unroll
+                for (int k = 1; k < kEach; ++k) m = fmaxf(m, v[k]);
+                if (m > above) pushed = push(v, first_index(c0 + t0 + j * kSelThreads + threadIdx.x), above);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) f += ex2_approx((v[k] - ref) * c);
+            }
+            full += static_cast<double>(f);
+            if (t0 + kTile >= n) break;
+            // a tighter bound each time the list has doubled
+            if (__syncthreads_or(pushed >= limit)) {
+                const int have = s.list_n;                        // (nobody adds to it here)
+                if (have > kListCap) { overflow = true; break; }
+                __syncthreads();
+                if (have > K) thr = fmaxf(thr, bound([&](int i) { return value_of(s.list[i]); }, have, K));
+                if (have > kListPrune) drop_below(thr, have);
+                limit = min(2 * s.list_n, kListPrune);
+                __syncthreads();
+            }
+        }
+        ends(true, thr);
+        __syncthreads();
+        overflow |= s.list_n > kListCap;
+        if (C == 1) return overflow ? -1 : sort_top(s.list_n, K);
+        // the K largest of every slice, sorted together by rank 0
+        const int mine = overflow ? -1 : sort_top(s.list_n, K);
+        if (threadIdx.x == 0) { s.pub.count = mine; s.pub.top = ref; }
         sync();
-        for (int j = 0; j < 3; ++j) sum[j] = 0;
-        before = 0;
-        n_sum = 0;
-        f_sum = 0.0;
+        int at = 0, all = 0;
         for (int r = 0; r < C; ++r) {
-            const Published* p = remote(&s.pub, r);
-            if (r < rank) before += p->mass[0];
-            sum[0] += p->mass[0];
-            sum[1] += p->mass[1];
-            n_sum += p->count;
-            f_sum += p->full;
+            const int k = remote(&s.pub, r)->count;
+            if (k < 0) overflow = true;
+            if (r < rank) at += k;
+            all += k;
+        }
+        // every CTA's sum about the reference of rank 0
+        const float ref0 = remote(&s.pub, 0)->top;
+        full *= exp2(static_cast<double>((ref - ref0) * c));
+        ref = ref0;
+        if (!overflow && rank != 0) {
+            u64* list = remote(s.list, 0) + at;
+            for (int i = threadIdx.x; i < mine; i += kSelThreads) list[i] = s.list[i];
         }
         sync();
+        if (overflow) return -1;
+        return rank != 0 ? 0 : sort_top(all, K);
     }
 };
 
-__device__ __forceinline__ float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// The slice [begin, begin + n) of a row to shared memory, 16 bytes at a time where they lie inside it; returns its largest value and
-// whether it holds a NaN or +inf.  An element keeps its place modulo 16 bytes, so `data` starts up to 15 bytes into the buffer.
-template <typename T>
-__device__ const T* load_slice(const T* src, int n, unsigned char* buf, float& top, int& bad) {
-    constexpr int kEach = 16 / sizeof(T);
-    const int mis = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
-    T* data = reinterpret_cast<T*>(buf) + mis;
-    const int chunks = (mis + n + kEach - 1) / kEach;
-    top = -INFINITY;
-    bad = 0;
-    auto see = [&](T v) {
-        const float x = to_f32(v);
-        if (!(x < INFINITY)) bad = 1;
-        top = fmaxf(top, x);
-    };
-    constexpr int kDeep = 4;
-    for (int c0 = threadIdx.x; c0 < chunks; c0 += kSelThreads * kDeep) {
-        uint4 v[kDeep];
-#pragma unroll
-        for (int j = 0; j < kDeep; ++j) {
-            const int c = c0 + j * kSelThreads, e = c * kEach - mis;
-            if (c < chunks && e >= 0 && e + kEach <= n) v[j] = __ldcs(reinterpret_cast<const uint4*>(src + e));
-        }
-#pragma unroll
-        for (int j = 0; j < kDeep; ++j) {
-            const int c = c0 + j * kSelThreads, e = c * kEach - mis;
-            if (c >= chunks) break;
-            if (e >= 0 && e + kEach <= n) {
-                const T* t = reinterpret_cast<const T*>(&v[j]);
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) see(t[k]);
-                reinterpret_cast<uint4*>(buf)[c] = v[j];
-            } else {
-                for (int k = 0; k < kEach; ++k)
-                    if (e + k >= 0 && e + k < n) {
-                        data[e + k] = src[e + k];
-                        see(data[e + k]);
-                    }
-            }
-        }
-    }
-    return data;
-}
-
-// Opens a row: slice, maximum, scale.  False where the row has no finite entry or holds a NaN or +inf (`what` says which).
-template <typename T>
-__device__ bool open_row(Row<T>& r, const SelectArgs& a, int64_t row, unsigned char* buf, float temperature, uint32_t& what) {
-    float top;
-    int bad;
-    r.begin = min(r.rank * a.slice, a.V);
-    r.n = min(a.slice, a.V - r.begin);
-    r.data = load_slice(static_cast<const T*>(a.x) + row * a.ld + r.begin, r.n, buf, top, bad);
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    bad = __any_sync(0xffffffffu, bad);
+// The first min(k, n) entries of the sorted list in rank 0: masses ahead of every entry give top-p, the value min-p; then the token by
+// the masses in the order of the indices.
+template <typename T, typename Write>
+__device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Write write) {
     SelShared& s = r.s;
-    if ((threadIdx.x & 31) == 0) {
-        s.warp_f64[threadIdx.x >> 5] = top;
-        s.warp_int[threadIdx.x >> 5] = bad;
+    constexpr int kMine = kMaxTopLogits / kSelThreads;
+    r.set_scale(value_of(s.list[0]), r.inv_t);
+    u64* w_of = reinterpret_cast<u64*>(s.hist);               // hist and tot: 2,048 words of 64 bits
+    static_assert(sizeof(s.hist) + sizeof(s.tot) >= kMaxTopLogits * sizeof(u64), "masses of the list");
+    u64 w[kMine], mine = 0, total;
+    const int i0 = threadIdx.x * kMine;
+    for (int j = 0; j < kMine; ++j) mine += w[j] = i0 + j < n ? r.mass(value_of(s.list[i0 + j])) : 0;
+    u64 cum = block_scan(mine, s.warp_u64[0], total);
+    const double target = static_cast<double>(p) * static_cast<double>(total), md = m;
+    int kept = 0;
+    for (int j = 0; j < kMine; ++j) {
+        const int i = i0 + j;
+        if (i < n && (i == 0 || ((p >= 1.f || static_cast<double>(cum) < target) && (!(m > 0.f) || value_of(s.list[i]) == r.top || r.weight(s.exp2_table, value_of(s.list[i])) >= md)))) ++kept;
+        cum += w[j];
     }
-    for (int b = threadIdx.x; b < kBins; b += kSelThreads) s.hist[b] = 0;
+    int n_kept;
+    block_scan(kept, s.warp_int, n_kept);
+    mine = 0;
+    for (int j = 0; j < kMine; ++j) {
+        w_of[i0 + j] = w[j];
+        if (i0 + j < n_kept) mine += w[j];
+    }
+    block_scan(mine, s.warp_u64[0], total);
+    const u64 t = __double2ull_rd(static_cast<double>(u) * static_cast<double>(total));
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 0; w < kSelWarps; ++w) {
-            top = fmaxf(top, static_cast<float>(s.warp_f64[w]));
-            bad |= s.warp_int[w];
-        }
-        s.pub.max = top;
-        s.pub.bad = bad;
+    for (int i = threadIdx.x; i < n_kept; i += kSelThreads) {
+        const int v = index_of(s.list[i]);
+        u64 c = 0;
+        for (int j = 0; j < n_kept; ++j)
+            if (index_of(s.list[j]) < v) c += w_of[j];
+        if (c <= t && t < c + w_of[i]) write(s.list[i], log(static_cast<double>(total) / kMassOne), n_kept);
     }
-    r.sync();
-    top = -INFINITY;
-    bad = 0;
-    for (int k = 0; k < r.C; ++k) {
-        const Published* p = r.remote(&s.pub, k);
-        top = fmaxf(top, p->max);
-        bad |= p->bad;
-    }
-    r.sync();
-    what = bad ? AIS_FLAG_NONFINITE : top == -INFINITY ? AIS_FLAG_EMPTY : 0u;
-    r.sc.top = top;
-    r.sc.inv_t = 1.0 / static_cast<double>(temperature);
-    r.sc.bins = kBinsPerNat / temperature;
-    r.sc.log2_scale = static_cast<float>(1.4426950408889634 * r.sc.inv_t);
-    return what == 0u;
-}
-
-// Histogram of the whole row and the fp32 sum of its exponentials (per thread).
-template <typename T>
-__device__ float histogram(const Row<T>& r) {
-    float full = 0.f;
-    r.each([&](float x, int) {
-        if (x == -INFINITY) return;
-        atomicAdd(&r.s.hist[r.sc.bin(x)], 1u);
-        full += ex2_approx((x - r.sc.top) * r.sc.log2_scale);
-    });
-    return full;
 }
 
 template <typename T>
@@ -533,10 +915,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     SelShared& s = *reinterpret_cast<SelShared*>(smem);
     pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
-    Row<T> r{s, nullptr, 0, 0, a.cluster, static_cast<int>(blockIdx.x % a.cluster), Scale()};
-    const bool first = r.rank == 0 && threadIdx.x == 0;
+    Row<T> r(s, a, row, static_cast<int>(blockIdx.x % a.cluster));
+    constexpr int kEach = Row<T>::kEach;
     auto neutral = [&](uint32_t flag) {
-        if (!first) return;
+        if (r.rank != 0 || threadIdx.x != 0) return;
         a.tokens[row] = -1;
         if (a.lp) a.lp[row] = 0.f;
         if (a.lp_full) a.lp_full[row] = 0.f;
@@ -545,7 +927,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     };
     if (a.mask && a.mask[row] == 0) return neutral(0u);
     float temperature = a.how.temperature_rows ? a.how.temperature_rows[row] : a.how.temperature;
-    int64_t k = a.how.top_k_rows ? a.how.top_k_rows[row] : a.how.top_k;
+    int k = a.how.top_k_rows ? a.how.top_k_rows[row] : a.how.top_k;
     const float p = a.how.top_p_rows ? a.how.top_p_rows[row] : a.how.top_p;
     const float m = a.how.min_p_rows ? a.how.min_p_rows[row] : a.how.min_p;
     const float u = a.u[row];
@@ -555,173 +937,287 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         temperature = 1.f;
         k = 1;
     }
-    uint32_t what;
-    if (!open_row(r, a, row, smem + sizeof(SelShared), temperature, what)) return neutral(what);
-    const Scale sc = r.sc;
-
-    const float full_thread = histogram(r);
-    const u64 none[3] = {0, 0, 0};
-    u64 sum[3], before;
-    int n_fin;
-    double full;
     {
-        int finite = 0;
-        r.each([&](float x, int) { finite += x != -INFINITY; });
-        r.add_up(none, finite, static_cast<double>(full_thread), sum, before, n_fin, full);
+        const double e = exp2((threadIdx.x >> 3) / 64.0);
+        static_assert(kSelThreads == 64 * 8 && kTableCopies == 16, "eight threads write the copies of an entry");
+        s.exp2_table[2 * threadIdx.x] = e;
+        s.exp2_table[2 * threadIdx.x + 1] = e;
     }
-    if (k <= 0 || k >= n_fin) k = n_fin;
-    const bool by_k = k < n_fin, by_p = p < 1.f;
-    const double pd = p, md = m;
-    auto above_m = [&](float x) { return !(m > 0.f) || x == sc.top || exp(sc.logw(x)) >= md; };
-    auto write = [&](u64 o, u64 total, int kept) {
-        const double logw = sc.logw(value_of(o));
+    __syncthreads();
+    r.inv_t = 1.0 / static_cast<double>(temperature);
+    const bool by_p = p < 1.f, by_m = m > 0.f;
+    const double pd = p, md = m, ud = u;
+    // what a row gives: log_full and log_total are relative to `about`
+    float about = 0.f;
+    double log_full = 0.0;
+    auto write = [&](u64 o, double log_total, int kept) {
+        const double x = static_cast<double>(value_of(o));
         a.tokens[row] = index_of(o);
-        if (a.lp) a.lp[row] = static_cast<float>(logw - log(static_cast<double>(total) / kMassOne));
-        if (a.lp_full) a.lp_full[row] = static_cast<float>(logw - log(full));
+        if (a.lp) a.lp[row] = static_cast<float>((x - static_cast<double>(r.top)) * r.inv_t - log_total);
+        if (a.lp_full) a.lp_full[row] = static_cast<float>((x - static_cast<double>(about)) * r.inv_t - log_full);
         if (a.n_kept) a.n_kept[row] = kept;
     };
 
-    if (by_k || by_p) r.merge_hist(false);
-    u64 cut = last_finite();
-    if (by_k) {
-        r.find_count(k);
-        const int bin = static_cast<int>(s.found[0]), ahead = static_cast<int>(s.found[1]), in = static_cast<int>(s.found[2]);
-        __syncthreads();
-        if (k <= kMaxTopLogits) {
-            int n_list;
-            if (ahead + in <= kListCap) {
-                n_list = r.gather_sorted([&](float x, u64) { return x != -INFINITY && sc.bin(x) <= bin; });
-            } else {
-                cut = r.template cut_in_group<false>([&](float x, u64) { return x != -INFINITY && sc.bin(x) == bin; }, in, k - ahead, 0, 0.0);
-                n_list = r.gather_sorted([&](float, u64 o) { return o <= cut; });
-            }
+    if (k > 0 && k <= kMaxTopLogits && k * r.C <= kListCap) {
+        double full;
+        const int n = r.stream_top(k, r.inv_t, about, full);
+        const double all = r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0];
+        if (n >= 0 && all > 0.0 && all < INFINITY) {
             if (r.rank != 0) return;
-            // the first k of the list: masses ahead of every entry give top-p, the value min-p; then the masses by index
-            constexpr int kEach = kMaxTopLogits / kSelThreads;
-            const int n1 = min(static_cast<int>(k), n_list);
-            u64 w[kEach], mine = 0, total;
-            const int i0 = threadIdx.x * kEach;
-            for (int j = 0; j < kEach; ++j) mine += w[j] = i0 + j < n1 ? sc.mass(value_of(s.list[i0 + j])) : 0;
-            u64 cum = block_scan(mine, s.warp_u64, total);
-            const double target = pd * static_cast<double>(total);
-            int kept = 0;
-            for (int j = 0; j < kEach; ++j) {
-                const int i = i0 + j;
-                if (i < n1 && (i == 0 || ((!by_p || static_cast<double>(cum) < target) && above_m(value_of(s.list[i]))))) ++kept;
-                cum += w[j];
-            }
-            int n_kept;
-            block_scan(kept, s.warp_int, n_kept);
-            mine = 0;
-            for (int j = 0; j < kEach; ++j) {
-                s.mass[i0 + j] = w[j];
-                if (i0 + j < n_kept) mine += w[j];
-            }
-            block_scan(mine, s.warp_u64, total);
-            const u64 t = __double2ull_rd(static_cast<double>(u) * static_cast<double>(total));
-            __syncthreads();
-            for (int i = threadIdx.x; i < n_kept; i += kSelThreads) {
-                const int v = index_of(s.list[i]);
-                u64 c = 0;
-                for (int j = 0; j < n_kept; ++j)
-                    if (index_of(s.list[j]) < v) c += s.mass[j];
-                if (c <= t && t < c + s.mass[i]) write(s.list[i], total, n_kept);
-            }
-            return;
-        }
-        cut = r.template cut_in_group<false>([&](float x, u64) { return x != -INFINITY && sc.bin(x) == bin; }, in, k - ahead, 0, 0.0);
-    }
-    if (by_p) {
-        if (by_k) {                                     // the histogram of what top-k has left
-            r.clear_hist(false);
-            r.each([&](float x, int i) {
-                if (order_of(x, r.begin + i) <= cut) atomicAdd(&s.hist[sc.bin(x)], 1u);
-            });
-            r.merge_hist(false);
-        }
-        // Bounds on the mass down to every bin from its counts: e^(-b / 64) and e^(-(b + 1) / 64) per entry, a thousandth apart from
-        // that for the rounding of the bins.  The cut lies in none of the bins before b1 and none behind b2.
-        int b1, b2;
-        {
-            double hi[kBinsPerThread], lo[kBinsPerThread], hs = 0.0, ls = 0.0, h_total, l_total;
-            const int b0 = threadIdx.x * kBinsPerThread;
-            for (int j = 0; j < kBinsPerThread; ++j) {
-                const double c = s.tot[b0 + j], e = exp(-(b0 + j) / 64.0);
-                hs += hi[j] = c * e * 1.001;
-                ls += lo[j] = b0 + j == kBins - 1 ? 0.0 : c * e * 0.983;            // e^(-1 / 64) = 0.9845
-            }
-            double h = block_scan(hs, s.warp_f64, h_total);
-            double l = block_scan(ls, s.warp_f64, l_total);
-            int n1 = 0, n2 = 0, total;
-            for (int j = 0; j < kBinsPerThread; ++j) {
-                h += hi[j];
-                l += lo[j];
-                n1 += h < pd * l_total;
-                n2 += l < pd * h_total;
-            }
-            block_scan(n1, s.warp_int, total);
-            b1 = min(total, kBins - 1);
-            block_scan(n2, s.warp_int, total);
-            b2 = min(total, kBins - 1);
-        }
-        for (int b = threadIdx.x; b < kBins; b += kSelThreads) s.mass[b] = 0;
-        __syncthreads();
-        u64 mine[3] = {0, 0, 0};
-        r.each([&](float x, int i) {
-            if (order_of(x, r.begin + i) > cut) return;
-            const u64 w = sc.mass(x);
-            const int b = sc.bin(x);
-            mine[0] += w;
-            if (b < b1) mine[1] += w;
-            else if (b <= b2) atomicAdd(&s.mass[b], w);
-        });
-        int n_none;
-        double f_none;
-        r.add_up(mine, 0, 0.0, sum, before, n_none, f_none);
-        const double target = pd * static_cast<double>(sum[0]);
-        r.merge_hist(true);                             // (the counts again: they have not changed)
-        r.find_mass(sum[1], target);
-        if (s.found[3] != 0) {
-            const int bin = static_cast<int>(s.found[0]), in = static_cast<int>(s.found[2]);
-            const u64 mass0 = s.found[1], all = cut;
-            __syncthreads();
-            cut = r.template cut_in_group<true>([&](float x, u64 o) { return o <= all && sc.bin(x) == bin; }, in, 0, mass0, target);
-        } else if (target <= 0.0) {
-            cut = order_of(sc.top, a.V);                // p = 0: the largest value; its first entry below
+            log_full = log(all);
+            return draw_from_list(r, n, p, m, u, write);
         }
     }
-    // The kept entries by index.
-    u64 mine[3] = {0, 0, 0};
+
+    typename Row<T>::Totals t;
+    u64 cut = last_finite();
     int kept = 0;
-    const bool only_first = by_p && p == 0.f;
-    r.each([&](float x, int i) {
-        if (order_of(x, r.begin + i) > cut || !above_m(x)) return;
-        mine[0] += sc.mass(x);
-        ++kept;
-    });
-    double f_none;
-    r.add_up(mine, kept, 0.0, sum, before, kept, f_none);
-    u64 t = __double2ull_rd(static_cast<double>(u) * static_cast<double>(sum[0]));
-    if (only_first) { t = 0; sum[0] = static_cast<u64>(kMassOne); kept = 1; }
-    // (s.warp_u64 still holds the masses of this CTA's warps)
-    if (t < before) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int w = 0; w < warp; ++w) before += s.warp_u64[w];
-    if (t < before || t >= before + s.warp_u64[warp]) return;
-    const int seg = r.segment(), from = warp * seg, to = min(from + seg, r.n);
-    for (int i0 = from; i0 < to; i0 += 32) {
-        const int i = i0 + lane;
-        const float x = i < to ? r.at(i) : -INFINITY;
-        const u64 o = order_of(x, r.begin + i);
-        const u64 w = i < to && o <= cut && above_m(x) ? sc.mass(x) : 0;
-        const u64 inc = before + warp_scan(w);
-        const unsigned hit = __ballot_sync(0xffffffffu, inc > t);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (k <= 0 && !by_p && !by_m) {
+        // Everything is kept: the sums about 0, or about the maximum where that leaves the range of fp64.
+        double about_d = 0.0;
+        for (int again = 0;; ++again) {
+            r.weight.set(r.inv_t, about_d);
+            double sum = 0.0;
+            float top = -INFINITY, least = INFINITY;
+            r.each([&](const float (&v)[kEach], int i, int n) {
+                float mn = v[0];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    top = max_nan(top, v[j]);
+                    mn = fminf(mn, v[j]);
+                }
+                if (n == kEach) least = fminf(least, mn);
+                if (mn >= r.weight.floor) {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) sum += r.weight.of(s.exp2_table, v[j]);
+                } else {
+                    for (int j = 0; j < n; ++j) least = fminf(least, to_f32(r.x[i + j]));
+#pragma unroll 1
+                    for (int j = 0; j < kEach; ++j) {
+                        float x = v[0];
+#pragma unroll
+                        for (int q = 1; q < kEach; ++q) x = q == j ? v[q] : x;
+                        sum += r.weight(s.exp2_table, x);
+                    }
+                }
+            });
+            const double of_warp = warp_sum(sum);
+            if (lane == 0) s.warp_kept[warp] = of_warp;
+            t = r.extremes(sum, top, least);
+            if (again || t.bad || t.top == -INFINITY || fabs(t.top * r.inv_t) < 600.0) break;
+            about_d = t.top;
+        }
+        if (t.bad || t.top == -INFINITY) return neutral(t.bad ? AIS_FLAG_NONFINITE : AIS_FLAG_EMPTY);
+        about = r.top = static_cast<float>(about_d);
+        log_full = log(t.sum[0]);
+        kept = t.count;
+    } else {
+        t = r.look();
+        if (t.bad || t.top == -INFINITY) return neutral(t.bad ? AIS_FLAG_NONFINITE : AIS_FLAG_EMPTY);
+        r.set_scale(t.top, r.inv_t);
+        about = t.top;
+        const bool by_k = k > 0 && k < t.count;
+        double full = 0.0;
+        if (by_k || by_p) full = r.histogram();
+        if (by_k) {
+            r.find_count(k);
+            const int b = s.found[0], ahead = s.found[1], in = s.found[2];
+            __syncthreads();
+            if (k <= kMaxTopLogits) {
+                log_full = log(r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0]);
+                int n;
+                if (ahead + in <= kListCap) {
+                    n = r.gather_sorted([&](float x, u64) { return x > -INFINITY && r.bin(x) <= b; });
+                } else {
+                    cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
+                    n = r.gather_sorted([&](float, u64 o) { return o <= cut; });
+                }
+                if (r.rank != 0) return;
+                return draw_from_list(r, min(n, k), p, m, u, write);
+            }
+            cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
+        }
+        // is an entry ahead of the cut, or it
+        float cut_value = value_of(cut);
+        int cut_index = index_of(cut);
+        auto inside = [&](float x, int i) { return x > cut_value || (x == cut_value && i <= cut_index); };
+        int b1 = 0;
+        double above = 0.0;                                       // mass of this thread's entries in the bins below b1
+        if (by_p) {
+            if (by_k) {                                           // the histogram of what top-k has left
+                r.clear_hist(false);
+                r.each([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j)
+                        if (inside(v[j], i + j)) atomicAdd(&s.hist[r.bin(v[j])], 1u);
+                });
+                r.merge_hist(false);
+            }
+            // Bounds on the mass down to every bin from its counts: e^(-b / 64) and e^(-(b + 1) / 64) per entry, a thousandth apart
+            // from that for the rounding of the bins.  The cut lies in none of the bins before b1 and none behind b2.
+            int b2;
+            {
+                double hi[kBinsPerThread], lo[kBinsPerThread], hs = 0.0, ls = 0.0, h_total, l_total;
+                const int b0 = threadIdx.x * kBinsPerThread;
+                for (int j = 0; j < kBinsPerThread; ++j) {
+                    const double c = r.counts()[b0 + j], e = exp(-(b0 + j) / 64.0);
+                    hs += hi[j] = c * e * 1.001;
+                    ls += lo[j] = b0 + j == kBins - 1 ? 0.0 : c * e * 0.983;            // e^(-1 / 64) = 0.9845
+                }
+                double h = block_scan(hs, s.warp_f64[0], h_total);
+                double l = block_scan(ls, s.warp_f64[0], l_total);
+                int n1 = 0, n2 = 0, total;
+                for (int j = 0; j < kBinsPerThread; ++j) {
+                    h += hi[j];
+                    l += lo[j];
+                    n1 += h < pd * l_total;
+                    n2 += l < pd * h_total;
+                }
+                block_scan(n1, s.warp_int, total);
+                b1 = min(total, kBins - 1);
+                block_scan(n2, s.warp_int, total);
+                b2 = min(total, kBins - 1);
+            }
+            for (int b = threadIdx.x; b < kBins; b += kSelThreads) s.mass[b] = 0;
+            __syncthreads();
+            double all = 0.0;
+            r.each([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    if (!inside(v[j], i + j)) continue;
+                    const double w = r.weight(s.exp2_table, v[j]);
+                    const int b = r.bin(v[j]);
+                    all += w;
+                    if (b < b1) above += w;
+                    else if (b <= b2) atomicAdd(&s.mass[b], __double2ull_rn(w * kMassOne));
+                }
+            });
+            t = r.template add_up<false>(all, above, 0, 0.f, 0);
+            const double target = pd * t.sum[0] * kMassOne;
+            r.merge_hist(true);                             // (the counts again: they have not changed)
+            r.find_mass(t.sum[1] * kMassOne, target);
+            if (s.found[3] != 0) {
+                const int b = s.found[0], in = s.found[2];
+                const double mass0 = s.found_mass;
+                __syncthreads();
+                cut = r.template cut_in_group<true>(
+                    [&](float x, u64 o) { return inside(x, index_of(o)) && r.bin(x) == b; }, in, 0, mass0, target);
+            } else if (target <= 0.0) {
+                cut = order_of(r.top, (1 << kIndexBits) - 1);                 // p = 0: the largest value
+            }
+            cut_value = value_of(cut);
+            cut_index = index_of(cut);
+        }
+        // The kept entries: those in the bins below b1 have been added up.  min-p takes its entries one by one.
+        const double m_from = by_m ? static_cast<double>(r.top) + log(md) / r.inv_t : 0.0;
+        const float m_floor = by_m ? static_cast<float>(m_from - 1e-6 * (fabs(static_cast<double>(r.top)) + fabs(m_from)) - 1e-30) : -INFINITY;
+        if (by_m) {
+            b1 = 0;
+            above = 0.0;
+        }
+        const float c = static_cast<float>(1.4426950408889634 * r.inv_t);
+        const bool sum_full = !by_k && !by_p;
+        r.each([&](const float (&v)[kEach], int i, int) {
+            float f = 0.f;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (sum_full) f += ex2_approx((v[j] - r.top) * c);
+                if (v[j] < m_floor || !inside(v[j], i + j)) continue;
+                if (r.bin(v[j]) >= b1) {
+                    const double w = r.weight(s.exp2_table, v[j]);
+                    if (by_m && w < md && v[j] != r.top) continue;
+                    above += w;
+                }
+                ++kept;
+            }
+            if (sum_full) full += static_cast<double>(f);
+        });
+        const double of_warp = warp_sum(above);
+        if (lane == 0) s.warp_kept[warp] = of_warp;
+        t = r.template add_up<false>(above, full, kept, 0.f, 0);
+        log_full = log(t.sum[1]);
+        kept = t.count;
+        if (by_p && p == 0.f) {                                   // ties of the largest value: the first of them alone
+            kept = 1;
+            t.sum[0] = 1.0;
+        }
+    }
+    // The token: the CTA, the warp and the entry at which the kept mass exceeds u times its total.  Sums of the same terms in another
+    // order may differ in their last bits, so the last candidate of each step takes what is left.
+    const bool first_only = by_p && p == 0.f;
+    const double want = first_only ? 0.0 : ud * t.sum[0];
+    // (t.before of the next CTA is this one's t.before + mine, the same sum: one CTA takes it)
+    if (threadIdx.x == 0) {
+        double mine = 0.0;
+        const double before = want - t.before;
+        int chosen = -1;
+        for (int w = 0; w < kSelWarps; ++w) mine += s.warp_kept[w];
+        s.found[0] = -1;
+        if (want >= t.before && mine > 0.0 && want < t.before + mine) {
+            double ahead = 0.0;
+            for (int w = 0; w < kSelWarps; ++w) {
+                if (s.warp_kept[w] <= 0.0) continue;
+                chosen = w;
+                s.found_mass = before - ahead;
+                if (before - ahead < s.warp_kept[w]) break;
+                ahead += s.warp_kept[w];
+            }
+            s.found[0] = chosen;
+        }
+    }
+    __syncthreads();
+    if (s.found[0] != warp) return;
+    const float cut_value = value_of(cut), m_top = r.top;
+    const int cut_index = index_of(cut);
+    double left = s.found_mass;
+    int from, to;
+    u64 last = ~0ull;                                             // the last entry with a mass (per lane)
+    r.range(from, to);
+    for (int base = from - 32; base < to + 32; base += 32) {      // the head of the row, the chunks, its tail
+        float v[kEach];
+        double w[kEach], sum = 0.0;
+        int i;
+        if (base < from || base >= to) {
+            if (!r.edge(base >= to, v, i)) continue;
+            if (lane > 0) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) v[j] = -INFINITY;
+            }
+        } else {
+            Elem<T>::unpack(r.chunk(base + lane, to), v);
+            i = r.first_index(base + lane);
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const bool in = v[j] > cut_value || (v[j] == cut_value && i + j <= cut_index);
+            w[j] = in ? r.weight(s.exp2_table, v[j]) : 0.0;
+            if (by_m && w[j] < md && v[j] != m_top) w[j] = 0.0;
+            sum += w[j];
+            if (w[j] > 0.0) last = order_of(v[j], i + j);
+        }
+        const double inc = warp_scan(sum);
+        const unsigned hit = __ballot_sync(0xffffffffu, inc > left);
         if (hit) {
-            if (lane == __ffs(hit) - 1) write(o, sum[0], kept);
+            if (lane == __ffs(hit) - 1) {
+                double at = inc - sum;
+                u64 o = last;
+#pragma unroll
+                for (int j = kEach - 1; j >= 0; --j) {            // the first whose sum exceeds what is left
+                    double c = at;
+                    for (int q = 0; q <= j; ++q) c += w[q];
+                    if (w[j] > 0.0 && c > left) o = order_of(v[j], i + j);
+                }
+                write(o, log(t.sum[0]), kept);
+            }
             return;
         }
-        before = __shfl_sync(0xffffffffu, inc, 31);
+        left -= __shfl_sync(0xffffffffu, inc, 31);
     }
+    // (rounding: the warp's last entry; the later index is the later lane's or chunk's)
+    int index = last == ~0ull ? -1 : index_of(last);
+    const int largest = __reduce_max_sync(0xffffffffu, index);
+    if (index == largest && index >= 0) write(last, log(t.sum[0]), kept);
 }
 
 template <typename T>
@@ -730,66 +1226,60 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
     SelShared& s = *reinterpret_cast<SelShared*>(smem);
     pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
-    Row<T> r{s, nullptr, 0, 0, a.cluster, static_cast<int>(blockIdx.x % a.cluster), Scale()};
-    auto fill = [&](int from) {
-        for (int i = from + threadIdx.x; i < a.K; i += kSelThreads) {
-            a.ids[row * a.ld_out + i] = -1;
-            a.values[row * a.ld_out + i] = -INFINITY;
+    Row<T> r(s, a, row, static_cast<int>(blockIdx.x % a.cluster));
+    auto write = [&](int n, float lse) {                          // n entries of the list, and padding
+        for (int i = threadIdx.x; i < a.K; i += kSelThreads) {
+            a.ids[row * a.ld_out + i] = i < n ? index_of(s.list[i]) : -1;
+            a.values[row * a.ld_out + i] = i < n ? value_of(s.list[i]) : -INFINITY;
         }
+        if (threadIdx.x == 0 && a.lse) a.lse[row] = lse;
     };
     auto neutral = [&](uint32_t flag, float lse) {
         if (r.rank != 0) return;
-        fill(0);
-        if (threadIdx.x != 0) return;
-        if (a.lse) a.lse[row] = lse;
-        if (flag && a.status) atomicOr(a.status, flag);
+        write(0, lse);
+        if (threadIdx.x == 0 && flag && a.status) atomicOr(a.status, flag);
     };
     if (a.mask && a.mask[row] == 0) return neutral(0u, 0.f);
-    uint32_t what;
-    if (!open_row(r, a, row, smem + sizeof(SelShared), a.tau, what)) return neutral(what, what == AIS_FLAG_EMPTY ? -INFINITY : NAN);
-    const Scale sc = r.sc;
-    const float full_thread = histogram(r);
-    const u64 none[3] = {0, 0, 0};
-    u64 sum[3], before;
-    int n_fin;
-    double full;
-    int finite = 0;
-    r.each([&](float x, int) { finite += x != -INFINITY; });
-    r.add_up(none, finite, static_cast<double>(full_thread), sum, before, n_fin, full);
-    r.merge_hist(false);
-    const int k = min(a.K, n_fin);
+    r.inv_t = 1.0 / static_cast<double>(a.tau);
+    if (a.K * r.C <= kListCap) {
+        float about;
+        double full;
+        const int n = r.stream_top(a.K, r.inv_t, about, full);
+        const double all = r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0];
+        if (n >= 0 && all > 0.0 && all < INFINITY) {
+            if (r.rank == 0) write(n, static_cast<float>(static_cast<double>(about) * r.inv_t + log(all)));
+            return;
+        }
+    }
+    const typename Row<T>::Totals t = r.look();
+    if (t.bad) return neutral(AIS_FLAG_NONFINITE, NAN);
+    if (t.top == -INFINITY) return neutral(AIS_FLAG_EMPTY, -INFINITY);
+    r.set_scale(t.top, r.inv_t);
+    const double full = r.template add_up<false>(r.histogram(), 0.0, 0, 0.f, 0).sum[0];
+    const int k = min(a.K, t.count);
     r.find_count(k);
-    const int bin = static_cast<int>(s.found[0]), ahead = static_cast<int>(s.found[1]), in = static_cast<int>(s.found[2]);
+    const int b = s.found[0], ahead = s.found[1], in = s.found[2];
     __syncthreads();
-    int n_list;
+    int n;
     if (ahead + in <= kListCap) {
-        n_list = r.gather_sorted([&](float x, u64) { return x != -INFINITY && sc.bin(x) <= bin; });
+        n = r.gather_sorted([&](float x, u64) { return x > -INFINITY && r.bin(x) <= b; });
     } else {
-        const u64 cut = r.template cut_in_group<false>([&](float x, u64) { return x != -INFINITY && sc.bin(x) == bin; }, in, k - ahead, 0, 0.0);
-        n_list = r.gather_sorted([&](float, u64 o) { return o <= cut; });
+        const u64 cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
+        n = r.gather_sorted([&](float, u64 o) { return o <= cut; });
     }
-    if (r.rank != 0) return;
-    for (int i = threadIdx.x; i < min(k, n_list); i += kSelThreads) {
-        a.ids[row * a.ld_out + i] = index_of(s.list[i]);
-        a.values[row * a.ld_out + i] = value_of(s.list[i]);
-    }
-    fill(min(k, n_list));
-    if (threadIdx.x == 0 && a.lse) a.lse[row] = static_cast<float>(static_cast<double>(sc.top) * sc.inv_t + log(full));
+    if (r.rank == 0) write(min(n, k), static_cast<float>(static_cast<double>(r.top) * r.inv_t + log(full)));
 }
 
 template <typename K>
 cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream) {
-    // Slices of 64 KB at most, so that two CTAs share an SM; more CTAs per row while the rows alone do not fill the GPU.
+    // More CTAs per row while the rows alone do not fill two CTAs per SM, and a slice keeps 16 KB.
     int c = 1;
-    while (c < kMaxCluster && (static_cast<int64_t>(a.V) * es > static_cast<int64_t>(c) * 64 * 1024 || (rows * c < 2 * 148 && a.V > c * 2048))) c *= 2;
+    while (c < kMaxCluster && rows * c < 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
     a.cluster = c;
-    a.slice = (((a.V + c - 1) / c) + 63) / 64 * 64;
-    const size_t smem = sizeof(SelShared) + static_cast<size_t>(a.slice) * es + 32;
-    static_assert(sizeof(SelShared) + kSliceBytes + 32 <= 227 * 1024, "shared memory of a CTA");
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rows * c));
     cfg.blockDim = dim3(kSelThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = sizeof(SelShared);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -822,7 +1312,7 @@ cudaError_t select_prepare() {
                              reinterpret_cast<const void*>(sample_kernel<float>),             reinterpret_cast<const void*>(top_logits_kernel<__nv_bfloat16>),
                              reinterpret_cast<const void*>(top_logits_kernel<__half>),        reinterpret_cast<const void*>(top_logits_kernel<float>)};
     for (const void* k : kernels) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SelShared)));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
