@@ -31,6 +31,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/ais.h"
 #include "host_setup.cuh"
 #include "launch.cuh"
@@ -44,18 +46,19 @@ namespace {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight, in the pass for the largest entries
-constexpr int kBatch = 2;                // and in the others, beside as many that are worked on
-constexpr int kBins = 2048;
-constexpr int kBinsPerThread = kBins / kSelThreads;
+constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight
+constexpr int kBins = 8192;
 constexpr int kListCap = 4096;           // entries of a list
+constexpr int kSplit = 1024;             // ways in which a group of entries is divided
 constexpr int kListPrune = 2048;         // a list is cut back beyond this
 constexpr int kRankSort = 256;           // entries up to which a list is sorted by counting
 constexpr int kMaxCluster = 8;
-constexpr float kBinsPerNat = 64.f;
+constexpr float kBinsPerNat = 256.f;
 constexpr int kIndexBits = 20;
 constexpr double kMassOne = 17592186044416.0;   // 2^44
 constexpr int kTableCopies = 16;         // of the table of powers of two
+
+constexpr float kTwo23 = 8388608.f;
 
 typedef unsigned long long u64;
 
@@ -67,18 +70,29 @@ struct Published {                       // what a CTA tells the others of its c
     int count;
 };
 
+// 72 KB: with two CTAs per SM this leaves 84 KB of L1, which the loads in flight need (at 105 KB the passes took three times as long).
 struct alignas(16) SelShared {
-    uint32_t hist[kBins];                // of this CTA's slice
-    uint32_t tot[kBins];                 // of the row (more than one CTA)
     union {
-        struct {
-            u64 mass[kBins];
-            u64 mass_tot[kBins];
-        };
+        uint32_t hist[kBins];            // of this CTA's slice; nobody needs it once there is a list
         u64 list[kListCap];
+        uint32_t indices[2 * kListCap];  // a list by index alone
+    };
+    union {
+        uint32_t tot[kBins];             // of the row (more than one CTA)
+        struct {
+            u64 mass[kSplit];            // dividing a group: masses and counts of this CTA, of the row (more than one CTA)
+            u64 mass_tot[kSplit];
+            uint32_t part[kSplit];
+            uint32_t part_tot[kSplit];
+        };
+        struct {
+            uint32_t small_hist[kSelThreads];
+            float group_max[2 * kSelThreads];
+        };
     };
     double exp2_table[64 * kTableCopies];   // 2^(j / 64)
     double warp_kept[kSelWarps];         // kept mass of every warp's range
+    u64 warp_listed[kSelWarps];          // what the list adds to it
     Published pub;
     double warp_f64[2][kSelWarps];
     u64 warp_u64[2][kSelWarps];
@@ -87,6 +101,9 @@ struct alignas(16) SelShared {
     int found[4];
     int list_n;
 };
+// (through the array itself and not through a pointer in a struct: the compiler then knows that it is shared memory)
+extern __shared__ __align__(16) unsigned char select_smem[];
+__device__ __forceinline__ SelShared& smem() { return *reinterpret_cast<SelShared*>(select_smem); }
 
 struct SelectArgs {
     const void* x;
@@ -166,6 +183,15 @@ __device__ __forceinline__ float ex2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// A 64-bit sum in shared memory by two 32-bit atomics: a 64-bit one is a loop of compare-and-swaps, which takes 300 us for the 2,000
+// entries of one value that share a sum.
+__device__ __forceinline__ void add_u64(u64* sum, u64 v) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(sum);
+    const uint32_t lo = static_cast<uint32_t>(v), old = atomicAdd(w, lo);
+    const uint32_t hi = static_cast<uint32_t>(v >> 32) + (old + lo < old ? 1u : 0u);
+    if (hi != 0u) atomicAdd(w + 1, hi);
 }
 
 template <typename N>
@@ -264,7 +290,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
 template <typename T>
 struct Row {
     static constexpr int kEach = Elem<T>::kEach;
-    SelShared& s;
     const T* x;              // the row
     int V, head;             // its length; elements before the first 16-byte boundary
     int whole;               // 16-byte chunks behind that
@@ -275,7 +300,7 @@ struct Row {
     double inv_t;
     Weight weight;           // about `top`
 
-    __device__ Row(SelShared& shared, const SelectArgs& a, int64_t row, int rank_) : s(shared), V(a.V), C(a.cluster), rank(rank_) {
+    __device__ Row(const SelectArgs& a, int64_t row, int rank_) : V(a.V), C(a.cluster), rank(rank_) {
         x = static_cast<const T*>(a.x) + row * a.ld;
         head = min(static_cast<int>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T)), V);
         whole = (V - head) / kEach;
@@ -311,26 +336,25 @@ struct Row {
         from = min(c0 + static_cast<int>(threadIdx.x >> 5) * per, c1);
         to = min(from + per, c1);
     }
-    // f(values, index of the first, how many are part of the row) for everything this warp owns, a thread at a time.  kBatch chunks are
-    // in flight while as many are worked on; the loop holds the code of no more (32 exponentials did not fit the instruction cache).
-    template <typename F>
+    // f(values, index of the first, how many are part of the row) for everything this warp owns, a thread at a time, B chunks of it in flight.
+    // A chunk's registers are loaded again as soon as it is unpacked: handing them on by moves would wait for the load.  B is 4 where
+    // f is short; with the exponentials 2 (four times eight of them did not fit the instruction cache).
+    template <int B, typename F>
     __device__ __forceinline__ void each(F f) const {
         int from, to;
         range(from, to);
         const int lane = threadIdx.x & 31;
-        uint4 raw[kBatch], next[kBatch];
+        uint4 raw[B];
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) raw[j] = chunk(from + lane + 32 * j, to);
+        for (int j = 0; j < B; ++j) raw[j] = chunk(from + lane + 32 * j, to);
 #pragma unroll 1
-        for (int c = from + lane; c < to; c += 32 * kBatch) {
+        for (int c = from + lane; c < to; c += 32 * B) {
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) next[j] = chunk(c + 32 * (kBatch + j), to);
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
+            for (int j = 0; j < B; ++j) {
                 float v[kEach];
                 Elem<T>::unpack(raw[j], v);
+                raw[j] = chunk(c + 32 * (B + j), to);
                 if (j == 0 || c + 32 * j < to) f(v, first_index(c + 32 * j), kEach);
-                raw[j] = next[j];
             }
         }
         // the ends of the row: lane 0 the head, lane 1 the tail
@@ -347,39 +371,35 @@ struct Row {
     }
     template <typename P>
     __device__ P* remote(P* p, int r) const { return C > 1 ? cg::this_cluster().map_shared_rank(p, r) : p; }
-    __device__ __forceinline__ int bin(float v) const {
-        const float y = (top - v) * bins;
-        return y < static_cast<float>(kBins - 1) ? static_cast<int>(y) : kBins - 1;
-    }
-    __device__ __forceinline__ u64 mass(float v) const { return __double2ull_rn(weight(s.exp2_table, v) * kMassOne); }
-    __device__ __forceinline__ const uint32_t* counts() const { return C > 1 ? s.tot : s.hist; }
-    __device__ __forceinline__ const u64* masses() const { return C > 1 ? s.mass_tot : s.mass; }
+    // The histogram bin of a value as a float above 2^23, whose low bits are the bin: the distance below the maximum in bins, rounded.
+    __device__ __forceinline__ float bin_f(float v) const { return fminf(fmaf(top - v, bins, kTwo23), kTwo23 + (kBins - 1)); }
+    __device__ __forceinline__ int bin(float v) const { return static_cast<int>(__float_as_uint(bin_f(v)) & (kBins - 1)); }
+    __device__ __forceinline__ u64 mass(float v) const { return __double2ull_rn(weight(smem().exp2_table, v) * kMassOne); }
+    __device__ __forceinline__ const uint32_t* counts() const { return C > 1 ? smem().tot : smem().hist; }
+    __device__ __forceinline__ const uint32_t* parts() const { return C > 1 ? smem().part_tot : smem().part; }
+    __device__ __forceinline__ const u64* masses() const { return C > 1 ? smem().mass_tot : smem().mass; }
 
-    __device__ void clear_hist(bool with_mass) const {
-        for (int b = threadIdx.x; b < kBins; b += kSelThreads) {
-            s.hist[b] = 0;
-            if (with_mass) s.mass[b] = 0;
-        }
+    __device__ void clear_hist() const {
+        SelShared& s = smem();
+        for (int b = threadIdx.x; b < kBins; b += kSelThreads) s.hist[b] = 0;
         __syncthreads();
     }
-    // hist (and mass) of all slices added up in every CTA
-    __device__ void merge_hist(bool with_mass) const {
-        sync();
-        if (C == 1) return;
-        const int share = kBins / C;
+    // An array of all slices added up in every CTA (C > 1); barriers around it are the caller's
+    template <typename N>
+    __device__ void merge(N* mine, N* total, int n) const {
+        const int share = n / C;
         for (int i = threadIdx.x; i < share; i += kSelThreads) {
             const int b = rank * share + i;
-            uint32_t c = 0;
-            u64 m = 0;
-            for (int r = 0; r < C; ++r) {
-                c += remote(s.hist, r)[b];
-                if (with_mass) m += remote(s.mass, r)[b];
-            }
-            for (int r = 0; r < C; ++r) {
-                remote(s.tot, r)[b] = c;
-                if (with_mass) remote(s.mass_tot, r)[b] = m;
-            }
+            N c = 0;
+            for (int r = 0; r < C; ++r) c += remote(mine, r)[b];
+            for (int r = 0; r < C; ++r) remote(total, r)[b] = c;
         }
+    }
+    __device__ void merge_hist() const {
+        SelShared& s = smem();
+        sync();
+        if (C == 1) return;
+        merge(s.hist, s.tot, kBins);
         sync();
     }
     // Two sums, a count and (with MAX) the largest value of all CTAs; `before`: sum[0] of the CTAs ahead of this one.
@@ -390,6 +410,7 @@ struct Row {
     };
     template <bool MAX>
     __device__ Totals add_up(double a, double b, int count, float top_, int bad) const {
+        SelShared& s = smem();
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         a = warp_sum(a);
         b = warp_sum(b);
@@ -436,35 +457,44 @@ struct Row {
         sync();
         return t;
     }
-    // The bin in which the count reaches k (k >= 1, no more than the total): s.found = {bin, entries before it, entries in it}.
-    __device__ void find_count(int k) const {
-        const int b0 = threadIdx.x * kBinsPerThread;
-        int c[kBinsPerThread], sum = 0, total;
-        for (int j = 0; j < kBinsPerThread; ++j) sum += c[j] = static_cast<int>(counts()[b0 + j]);
+    // The first of n counts, n a multiple of the threads, at which their sum reaches k (k >= 1, no more than the total): s.found = {which,
+    // entries before it, entries in it}.
+    template <int N>
+    __device__ void find_count(const uint32_t* count, int k) const {
+        SelShared& s = smem();
+        constexpr int kMine = N / kSelThreads;
+        const int b0 = threadIdx.x * kMine;
+        int sum = 0, total;
+        for (int j = 0; j < kMine; ++j) sum += static_cast<int>(count[b0 + j]);
         int before = block_scan(sum, s.warp_int, total);
-        for (int j = 0; j < kBinsPerThread; ++j) {
-            if (before < k && before + c[j] >= k) {
-                s.found[0] = b0 + j;
-                s.found[1] = before;
-                s.found[2] = c[j];
+        if (before < k && before + sum >= k) {
+            for (int j = 0; j < kMine; ++j) {
+                const int c = static_cast<int>(count[b0 + j]);
+                if (before < k && before + c >= k) {
+                    s.found[0] = b0 + j;
+                    s.found[1] = before;
+                    s.found[2] = c;
+                }
+                before += c;
             }
-            before += c[j];
         }
         __syncthreads();
     }
-    // The bin in which mass0 plus the masses reach the target: s.found = {bin, -, entries in it, whether there is one}, s.found_mass the
+    // The part in which mass0 plus the masses reach the target: s.found = {part, -, entries in it, whether there is one}, s.found_mass the
     // mass before it.
     __device__ void find_mass(double mass0, double target) const {
+        SelShared& s = smem();
         if (threadIdx.x == 0) s.found[3] = 0;
-        const int b0 = threadIdx.x * kBinsPerThread;
-        u64 m[kBinsPerThread], sum = 0, total;
-        for (int j = 0; j < kBinsPerThread; ++j) sum += m[j] = masses()[b0 + j];
+        constexpr int kMine = kSplit / kSelThreads;
+        const int b0 = threadIdx.x * kMine;
+        u64 m[kMine], sum = 0, total;
+        for (int j = 0; j < kMine; ++j) sum += m[j] = masses()[b0 + j];
         u64 before = block_scan(sum, s.warp_u64[0], total);
-        for (int j = 0; j < kBinsPerThread; ++j) {
+        for (int j = 0; j < kMine; ++j) {
             const double lo = mass0 + static_cast<double>(before), hi = mass0 + static_cast<double>(before + m[j]);
             if (m[j] != 0 && lo < target && hi >= target) {
                 s.found[0] = b0 + j;
-                s.found[2] = counts()[b0 + j];
+                s.found[2] = parts()[b0 + j];
                 s.found[3] = 1;
                 s.found_mass = lo;
             }
@@ -472,29 +502,85 @@ struct Row {
         }
         __syncthreads();
     }
-    // Entries that keep(value, order) takes go to the list of rank 0, sorted there; only rank 0 has it (and its length, at most kListCap).
+    // From the merged counts: the bins b1 .. b2 in which the mass can reach the target.  An entry of bin b weighs between e^(-(b + 1/2) / 256)
+    // and e^(-(b - 1/2) / 256), but for the rounding of the bin (1e-6 of a distance of 32) and of the exponentials here: 2e-5 to either side.
+    // Without a total the target is p times the sum, which is bounded alike; with it, bins before b0 weigh `mass0` together.
+    // s.found = {entries before b1, entries from b1 to b2}.
+    __device__ void bracket(double p, double total, double mass0, int from, int& b1, int& b2) const {
+        SelShared& s = smem();
+        constexpr int kMine = kBins / kSelThreads;
+        const int b0 = threadIdx.x * kMine;
+        const uint32_t* count = counts();
+        const float step = -1.4426950408889634f / kBinsPerNat;
+        double hs = 0.0, ls = 0.0, h_total, l_total;
+        for (int j = 0; j < kMine; ++j) {
+            const float c = static_cast<float>(count[b0 + j]);    // (exact below 2^24)
+            if (c == 0.f || b0 + j < from) continue;
+            hs += static_cast<double>(c * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f));
+            ls += b0 + j == kBins - 1 ? 0.0 : static_cast<double>(c * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
+        }
+        double h = mass0 + block_scan(hs, s.warp_f64[0], h_total);
+        double l = mass0 + block_scan(ls, s.warp_f64[0], l_total);
+        const double to_lo = p * (total > 0.0 ? total : l_total), to_hi = p * (total > 0.0 ? total : h_total);
+        int n1 = 0, n2 = 0;
+        for (int j = 0; j < kMine; ++j) {
+            const float c = static_cast<float>(count[b0 + j]);
+            if (c != 0.f && b0 + j >= from) {
+                h += static_cast<double>(c * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f));
+                l += b0 + j == kBins - 1 ? 0.0 : static_cast<double>(c * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
+            }
+            n1 += b0 + j < from || h < to_lo;
+            n2 += b0 + j < from || l < to_hi;
+        }
+        block_scan(n1, s.warp_int, b1);
+        b1 = min(b1, kBins - 1);
+        block_scan(n2, s.warp_int, b2);
+        b2 = min(b2, kBins - 1);
+        int before = 0, in = 0, sum;
+        for (int j = 0; j < kMine; ++j) {
+            const int c = static_cast<int>(count[b0 + j]);
+            if (b0 + j < b1) before += c;
+            else if (b0 + j <= b2) in += c;
+        }
+        block_scan(before, s.warp_int, sum);
+        if (threadIdx.x == 0) s.found[0] = sum;
+        block_scan(in, s.warp_int, sum);
+        if (threadIdx.x == 0) s.found[1] = sum;
+        __syncthreads();
+    }
+    // Entries that keep(value, index) takes, 4,096 at most, go to the list of rank 0; only rank 0 has it (and its length).
     template <typename F>
-    __device__ int gather_sorted(F keep) const {
-        sync();                                    // the list shares its place with the masses
+    __device__ int gather(F keep) const {
+        SelShared& s = smem();
+        sync();                                    // the list shares its place with the counts
         if (threadIdx.x == 0) s.list_n = 0;
         sync();
         int* counter = remote(&s.list_n, 0);
         u64* list = remote(s.list, 0);
-        each([&](const float (&v)[kEach], int i, int) {
+        each<kDeep>([&](const float (&v)[kEach], int i, int) {
+            unsigned taken = 0;
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) {
-                const u64 o = order_of(v[k], i + k);
-                if (keep(v[k], o)) {
+            for (int k = 0; k < kEach; ++k) taken |= (keep(v[k], i + k) ? 1u : 0u) << k;
+            if (taken == 0u) return;
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (taken >> k & 1u) {
                     const int at = atomicAdd(counter, 1);
-                    if (at < kListCap) list[at] = o;
+                    if (at < kListCap) list[at] = order_of(v[k], i + k);
                 }
-            }
         });
         sync();
-        if (rank != 0) return 0;
-        return sort_list(min(s.list_n, kListCap));
+        return rank == 0 ? min(s.list_n, 4096) : 0;
+    }
+    // Which warp of the CTA that has it owns the entry with this index (see range() and edge()).
+    __device__ __forceinline__ int warp_of(int index) const {
+        if (index < head) return 0;
+        const int c = (index - head) / kEach;
+        if (c >= whole) return kSelWarps - 1;
+        return (c - c0) / (((c1 - c0 + kSelWarps - 1) / kSelWarps + 31) / 32 * 32);
     }
     __device__ int sort_list(int n) const {
+        SelShared& s = smem();
         const int n2 = pow2_from(n);
         if (n <= kRankSort) {                                     // every entry counts those before it
             const u64 o = threadIdx.x < n ? s.list[threadIdx.x] : 0;
@@ -514,6 +600,7 @@ struct Row {
     // fewer than K are finite.  Histograms of 512 bins, each over the bin of the K-th value of the one before.
     template <typename F>
     __device__ float bound(F val, int n, int K, float* largest = nullptr) const {
+        SelShared& s = smem();
         float lo = INFINITY, hi = -INFINITY;
         auto extend = [&](float& l, float& h) {                   // over the block
             for (int o = 16; o > 0; o >>= 1) {
@@ -539,15 +626,15 @@ struct Row {
         for (int level = 0; level < 5; ++level) {
             const float scale = hi > lo ? fminf(511.9f / (hi - lo), 1e38f) : 0.f;
             static_assert(kSelThreads == 512, "a thread per bin");
-            s.hist[threadIdx.x] = 0;
+            s.small_hist[threadIdx.x] = 0;
             if (threadIdx.x == 0) s.found[0] = -1;
             __syncthreads();
             for (int i = threadIdx.x; i < n; i += kSelThreads) {
                 const float v = val(i);
-                if (v >= lo && v <= hi) atomicAdd(&s.hist[min(static_cast<int>((hi - v) * scale), 511)], 1u);
+                if (v >= lo && v <= hi) atomicAdd(&s.small_hist[min(static_cast<int>((hi - v) * scale), 511)], 1u);
             }
             __syncthreads();
-            const int c = static_cast<int>(s.hist[threadIdx.x]);
+            const int c = static_cast<int>(s.small_hist[threadIdx.x]);
             int total;
             const int before = ahead + block_scan(c, s.warp_int, total);
             if (before < K && before + c >= K) {
@@ -573,8 +660,9 @@ struct Row {
     }
     // The list without the entries below `thr`.
     __device__ void drop_below(float thr, int n) const {
-        constexpr int kMine = kListCap / kSelThreads;
-        u64 o[kMine];
+        SelShared& s = smem();
+        constexpr int kMine = 4096 / kSelThreads;
+        u64 o[kMine];                                             // (n <= 4096)
 #pragma unroll
         for (int j = 0; j < kMine; ++j) o[j] = threadIdx.x + j * kSelThreads < n ? s.list[threadIdx.x + j * kSelThreads] : ~0ull;
         __syncthreads();
@@ -587,6 +675,7 @@ struct Row {
     }
     // The K largest of the first n entries of the list, sorted; returns their number.
     __device__ int sort_top(int n, int K) const {
+        SelShared& s = smem();
         if (n > kRankSort && n > K + K / 4 + 8) {
             const float thr = bound([&](int i) { return value_of(s.list[i]); }, n, K);
             drop_below(thr, n);
@@ -595,99 +684,75 @@ struct Row {
         }
         return min(sort_list(n), K);
     }
-    // Smallest and largest number of the entries that pick(value, order) takes.
-    template <typename F>
-    __device__ void range_of(F pick, u64& lo, u64& hi) const {
-        u64 a = ~0ull, b = 0;
-        each([&](const float (&v)[kEach], int i, int) {
-#pragma unroll
-            for (int k = 0; k < kEach; ++k) {
-                const u64 o = order_of(v[k], i + k);
-                if (pick(v[k], o)) { a = min(a, o); b = max(b, o); }
+    // The cut inside a group of `count` entries, those that over(f) calls f(value, number) for, in all CTAs: by count, the entry number `want`
+    // (from 1) of the group; by mass, the first at which mass0 plus the masses reach `target` (in units of 2^-44).  The range of numbers is
+    // divided 1,024 ways, and again the part with the cut, until one number is left; by mass, the last of the group where rounding
+    // leaves none.  No list is touched.
+    template <bool MASS, typename Over>
+    __device__ u64 cut_in_group(Over over, int want, double mass0, double target) const {
+        SelShared& s = smem();
+        u64 lo = ~0ull, hi = 0;
+        over([&](float, u64 o) { lo = min(lo, o); hi = max(hi, o); });
+        for (;;) {
+            // what is left of the group, its ends
+            for (int o = 16; o > 0; o >>= 1) {
+                lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
             }
-        });
-        for (int o = 16; o > 0; o >>= 1) {
-            a = min(a, __shfl_xor_sync(0xffffffffu, a, o));
-            b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-        }
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = a; s.warp_u64[1][threadIdx.x >> 5] = b; }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 0; w < kSelWarps; ++w) { a = min(a, s.warp_u64[0][w]); b = max(b, s.warp_u64[1][w]); }
-            s.pub.lo = a;
-            s.pub.hi = b;
-        }
-        sync();
-        lo = ~0ull;
-        hi = 0;
-        for (int r = 0; r < C; ++r) {
-            lo = min(lo, remote(&s.pub, r)->lo);
-            hi = max(hi, remote(&s.pub, r)->hi);
-        }
-        sync();
-    }
-    // The cut inside a group of `count` entries, those that pick(value, order) takes: by count, the entry number `want` (from 1) of the
-    // group; by mass, the first at which mass0 plus the masses reach `target`.
-    template <bool MASS, typename F>
-    __device__ u64 cut_in_group(F pick, int count, int want, double mass0, double target) const {
-        if (count <= kListCap) return cut_in_list<MASS>(pick, want, mass0, target);
-        u64 lo, hi;
-        range_of(pick, lo, hi);
-        while (count > kListCap) {                               // (a single number is one entry)
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = lo; s.warp_u64[1][threadIdx.x >> 5] = hi; }
+            for (int b = threadIdx.x; b < kSplit; b += kSelThreads) {
+                s.part[b] = 0;
+                if (MASS) s.mass[b] = 0;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int w = 0; w < kSelWarps; ++w) { lo = min(lo, s.warp_u64[0][w]); hi = max(hi, s.warp_u64[1][w]); }
+                s.pub.lo = lo;
+                s.pub.hi = hi;
+            }
+            sync();
+            for (int r = 0; r < C; ++r) {
+                lo = min(lo, remote(&s.pub, r)->lo);
+                hi = max(hi, remote(&s.pub, r)->hi);
+            }
+            if (lo >= hi) {                                       // one number, or (a group without entries) none
+                sync();
+                return hi;
+            }
             const int bits = 64 - __clzll(hi - lo);
-            const int shift = bits > 11 ? bits - 11 : 0;
-            clear_hist(MASS);
-            each([&](const float (&v)[kEach], int i, int) {
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) {
-                    const u64 o = order_of(v[k], i + k);
-                    if (o < lo || o > hi) continue;
-                    const int b = static_cast<int>((o - lo) >> shift);
-                    atomicAdd(&s.hist[b], 1u);
-                    if (MASS) atomicAdd(&s.mass[b], mass(v[k]));
-                }
+            const int shift = bits > 10 ? bits - 10 : 0;
+            over([&](float x, u64 o) {
+                if (o < lo || o > hi) return;
+                const int b = static_cast<int>((o - lo) >> shift);
+                atomicAdd(&s.part[b], 1u);
+                if (MASS) add_u64(&s.mass[b], mass(x));
             });
-            merge_hist(MASS);
+            sync();
+            if (C > 1) {
+                merge(s.part, s.part_tot, kSplit);
+                if (MASS) merge(s.mass, s.mass_tot, kSplit);
+                sync();
+            }
             if (MASS) {
                 find_mass(mass0, target);
-                if (s.found[3] == 0) return hi;                  // rounding: the whole group
+                if (s.found[3] == 0) return hi;
                 mass0 = s.found_mass;
             } else {
-                find_count(want);
+                find_count<kSplit>(parts(), want);
                 want -= s.found[1];
             }
-            count = s.found[2];
-            lo += static_cast<u64>(s.found[0]) << shift;
-            hi = min(hi, lo + ((1ull << shift) - 1));
-            __syncthreads();
-        }
-        return cut_in_list<MASS>([=](float, u64 o) { return o >= lo && o <= hi; }, want, mass0, target);
-    }
-    template <bool MASS, typename F>
-    __device__ u64 cut_in_list(F pick, int want, double mass0, double target) const {
-        const int n_list = gather_sorted(pick);
-        if (rank == 0) {
-            if (MASS) {
-                constexpr int kMine = kListCap / kSelThreads;
-                u64 m[kMine], sum = 0, total;
-                const int i0 = threadIdx.x * kMine;
-                for (int j = 0; j < kMine; ++j) sum += m[j] = i0 + j < n_list ? mass(value_of(s.list[i0 + j])) : 0;
-                if (threadIdx.x == 0) s.pub.lo = s.list[n_list - 1];
-                u64 before = block_scan(sum, s.warp_u64[0], total);
-                for (int j = 0; j < kMine; ++j) {
-                    if (i0 + j < n_list && mass0 + static_cast<double>(before) < target && mass0 + static_cast<double>(before + m[j]) >= target)
-                        s.pub.lo = s.list[i0 + j];
-                    before += m[j];
-                }
-            } else if (threadIdx.x == 0) {
-                s.pub.lo = s.list[want - 1];
+            const u64 from = lo + (static_cast<u64>(s.found[0]) << shift), to = min(hi, from + ((1ull << shift) - 1));
+            if (shift == 0) {
+                sync();
+                return from;
             }
+            lo = ~0ull;
+            hi = 0;
+            over([&](float, u64 o) {
+                if (o >= from && o <= to) { lo = min(lo, o); hi = max(hi, o); }
+            });
         }
-        sync();
-        const u64 cut = remote(&s.pub, 0)->lo;
-        sync();
-        return cut;
     }
 
     __device__ void set_scale(float top_, double inv_t_) {
@@ -699,7 +764,7 @@ struct Row {
     // The row's maximum, number of finite entries and whether it holds a NaN or +inf.
     __device__ Totals look() const {
         float m = -INFINITY, least = INFINITY;
-        each([&](const float (&v)[kEach], int, int n) {
+        each<kDeep>([&](const float (&v)[kEach], int, int n) {
 #pragma unroll
             for (int k = 0; k < kEach; ++k) {
                 m = max_nan(m, v[k]);
@@ -714,7 +779,7 @@ struct Row {
         Totals t = add_up<true>(sum, 0.0, 0, isnan(m) ? -INFINITY : m, (m < INFINITY ? 0 : 1) | (least == -INFINITY ? 2 : 0));
         if ((t.bad & 2) != 0) {
             int finite = 0;
-            each([&](const float (&v)[kEach], int, int) {
+            each<kDeep>([&](const float (&v)[kEach], int, int) {
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) finite += v[k] > -INFINITY;
             });
@@ -725,31 +790,34 @@ struct Row {
         t.bad &= 1;
         return t;
     }
-    // Histogram of the row, merged; returns the fp32 sum of its exponentials about `top` (this thread's part).
+    // Histogram of the row, merged; with SUM also the fp32 sum of its exponentials about `top` (this thread's part).
+    template <bool SUM>
     __device__ double histogram() const {
+        SelShared& s = smem();
         const float c = static_cast<float>(1.4426950408889634 * inv_t);
-        clear_hist(false);
+        clear_hist();
         double full = 0.0;
-        each([&](const float (&v)[kEach], int, int) {
+        each<kDeep>([&](const float (&v)[kEach], int, int) {
             float f = 0.f;
 #pragma unroll
             for (int k = 0; k < kEach; ++k) {
                 if (v[k] > -INFINITY) atomicAdd(&s.hist[bin(v[k])], 1u);
-                f += ex2_approx((v[k] - top) * c);
+                if (SUM) f += ex2_approx((v[k] - top) * c);
             }
-            full += static_cast<double>(f);
+            if (SUM) full += static_cast<double>(f);
         });
-        merge_hist(false);
+        merge_hist();
         return full;
     }
 
     // The K largest entries by one pass: rank 0 gets them sorted in s.list and returns their number, and the fp32 sum of exponentials
     // about `ref` in `full` (all threads of all CTAs).  -1: the list overflowed, or the sum says that the row needs a closer look.
     __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
+        SelShared& s = smem();
         constexpr int kTile = kSelThreads * kDeep;
         const float c = static_cast<float>(1.4426950408889634 * inv_t_);
         const int n = c1 - c0;
-        float* group_max = reinterpret_cast<float*>(s.tot);       // 1,024 group maxima at most
+        float* group_max = s.group_max;
         if (threadIdx.x == 0) s.list_n = 0;
         __syncthreads();
         uint4 raw[kDeep];
@@ -814,13 +882,11 @@ struct Row {
             float f = 0.f;
             // (>= in the first tile, whose entries gave the bound; later ones of the same value come after K entries in the order)
             const float above = tile == 0 ? nextafterf(thr, -INFINITY) : thr;
-#pragma unroll 1
+#pragma unroll
             for (int j = 0; j < kDeep; ++j) {
                 float v[kEach];
-                Elem<T>::unpack(raw[0], v);
-#pragma unroll
-                for (int i = 0; i + 1 < kDeep; ++i) raw[i] = raw[i + 1];
-                raw[kDeep - 1] = chunk(c0 + t0 + (kDeep + j) * kSelThreads + threadIdx.x, c1);
+                Elem<T>::unpack(raw[j], v);
+                raw[j] = chunk(c0 + t0 + (kDeep + j) * kSelThreads + threadIdx.x, c1);
                 float m = v[0];
 #pragma unroll
                 for (int k = 1; k < kEach; ++k) m = fmaxf(m, v[k]);
@@ -833,7 +899,7 @@ struct Row {
             // a tighter bound each time the list has doubled
             if (__syncthreads_or(pushed >= limit)) {
                 const int have = s.list_n;                        // (nobody adds to it here)
-                if (have > kListCap) { overflow = true; break; }
+                if (have > 4096) { overflow = true; break; }
                 __syncthreads();
                 if (have > K) thr = fmaxf(thr, bound([&](int i) { return value_of(s.list[i]); }, have, K));
                 if (have > kListPrune) drop_below(thr, have);
@@ -843,7 +909,7 @@ struct Row {
         }
         ends(true, thr);
         __syncthreads();
-        overflow |= s.list_n > kListCap;
+        overflow |= s.list_n > 4096;
         if (C == 1) return overflow ? -1 : sort_top(s.list_n, K);
         // the K largest of every slice, sorted together by rank 0
         const int mine = overflow ? -1 : sort_top(s.list_n, K);
@@ -874,11 +940,11 @@ struct Row {
 // the masses in the order of the indices.
 template <typename T, typename Write>
 __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Write write) {
-    SelShared& s = r.s;
+    SelShared& s = smem();
     constexpr int kMine = kMaxTopLogits / kSelThreads;
     r.set_scale(value_of(s.list[0]), r.inv_t);
-    u64* w_of = reinterpret_cast<u64*>(s.hist);               // hist and tot: 2,048 words of 64 bits
-    static_assert(sizeof(s.hist) + sizeof(s.tot) >= kMaxTopLogits * sizeof(u64), "masses of the list");
+    u64* w_of = s.mass;
+    static_assert(kSplit >= kMaxTopLogits, "masses of the list");
     u64 w[kMine], mine = 0, total;
     const int i0 = threadIdx.x * kMine;
     for (int j = 0; j < kMine; ++j) mine += w[j] = i0 + j < n ? r.mass(value_of(s.list[i0 + j])) : 0;
@@ -911,11 +977,10 @@ __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Writ
 
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_constant__ SelectArgs a) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    SelShared& s = *reinterpret_cast<SelShared*>(smem);
+    SelShared& s = smem();
     pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
-    Row<T> r(s, a, row, static_cast<int>(blockIdx.x % a.cluster));
+    Row<T> r(a, row, static_cast<int>(blockIdx.x % a.cluster));
     constexpr int kEach = Row<T>::kEach;
     auto neutral = [&](uint32_t flag) {
         if (r.rank != 0 || threadIdx.x != 0) return;
@@ -958,7 +1023,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         if (a.n_kept) a.n_kept[row] = kept;
     };
 
-    if (k > 0 && k <= kMaxTopLogits && k * r.C <= kListCap) {
+    if (k > 0 && k <= kMaxTopLogits && k * r.C <= 4096) {
         double full;
         const int n = r.stream_top(k, r.inv_t, about, full);
         const double all = r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0];
@@ -980,7 +1045,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
             r.weight.set(r.inv_t, about_d);
             double sum = 0.0;
             float top = -INFINITY, least = INFINITY;
-            r.each([&](const float (&v)[kEach], int i, int n) {
+            r.template each<2>([&](const float (&v)[kEach], int i, int n) {
                 float mn = v[0];
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
@@ -1018,124 +1083,152 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         r.set_scale(t.top, r.inv_t);
         about = t.top;
         const bool by_k = k > 0 && k < t.count;
-        double full = 0.0;
-        if (by_k || by_p) full = r.histogram();
-        if (by_k) {
-            r.find_count(k);
-            const int b = s.found[0], ahead = s.found[1], in = s.found[2];
-            __syncthreads();
-            if (k <= kMaxTopLogits) {
-                log_full = log(r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0]);
-                int n;
-                if (ahead + in <= kListCap) {
-                    n = r.gather_sorted([&](float x, u64) { return x > -INFINITY && r.bin(x) <= b; });
-                } else {
-                    cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
-                    n = r.gather_sorted([&](float, u64 o) { return o <= cut; });
-                }
-                if (r.rank != 0) return;
-                return draw_from_list(r, min(n, k), p, m, u, write);
-            }
-            cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
-        }
+        double full = 0.0;                                        // sum of all exponentials (this thread's part)
+        if (by_k) full = r.template histogram<true>();
+        else if (by_p) r.template histogram<false>();
         // is an entry ahead of the cut, or it
         float cut_value = value_of(cut);
         int cut_index = index_of(cut);
         auto inside = [&](float x, int i) { return x > cut_value || (x == cut_value && i <= cut_index); };
-        int b1 = 0;
-        double above = 0.0;                                       // mass of this thread's entries in the bins below b1
-        if (by_p) {
-            if (by_k) {                                           // the histogram of what top-k has left
-                r.clear_hist(false);
-                r.each([&](const float (&v)[kEach], int i, int) {
+        // the entries of the slice that pick(value, index) takes, as cut_in_group wants them
+        auto data = [&](auto pick) {
+            return [&r, pick](auto f) {
+                r.template each<kDeep>([&](const float (&v)[kEach], int i, int) {
+                    unsigned taken = 0;
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) taken |= (pick(v[j], i + j) ? 1u : 0u) << j;
+                    if (taken == 0u) return;
 #pragma unroll
                     for (int j = 0; j < kEach; ++j)
-                        if (inside(v[j], i + j)) atomicAdd(&s.hist[r.bin(v[j])], 1u);
+                        if (taken >> j & 1u) f(v[j], order_of(v[j], i + j));
                 });
-                r.merge_hist(false);
-            }
-            // Bounds on the mass down to every bin from its counts: e^(-b / 64) and e^(-(b + 1) / 64) per entry, a thousandth apart
-            // from that for the rounding of the bins.  The cut lies in none of the bins before b1 and none behind b2.
-            int b2;
-            {
-                double hi[kBinsPerThread], lo[kBinsPerThread], hs = 0.0, ls = 0.0, h_total, l_total;
-                const int b0 = threadIdx.x * kBinsPerThread;
-                for (int j = 0; j < kBinsPerThread; ++j) {
-                    const double c = r.counts()[b0 + j], e = exp(-(b0 + j) / 64.0);
-                    hs += hi[j] = c * e * 1.001;
-                    ls += lo[j] = b0 + j == kBins - 1 ? 0.0 : c * e * 0.983;            // e^(-1 / 64) = 0.9845
-                }
-                double h = block_scan(hs, s.warp_f64[0], h_total);
-                double l = block_scan(ls, s.warp_f64[0], l_total);
-                int n1 = 0, n2 = 0, total;
-                for (int j = 0; j < kBinsPerThread; ++j) {
-                    h += hi[j];
-                    l += lo[j];
-                    n1 += h < pd * l_total;
-                    n2 += l < pd * h_total;
-                }
-                block_scan(n1, s.warp_int, total);
-                b1 = min(total, kBins - 1);
-                block_scan(n2, s.warp_int, total);
-                b2 = min(total, kBins - 1);
-            }
-            for (int b = threadIdx.x; b < kBins; b += kSelThreads) s.mass[b] = 0;
+            };
+        };
+        if (by_k) {
+            r.template find_count<kBins>(r.counts(), k);
+            const int b = s.found[0], ahead = s.found[1], in = s.found[2];
             __syncthreads();
-            double all = 0.0;
-            r.each([&](const float (&v)[kEach], int i, int) {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) {
-                    if (!inside(v[j], i + j)) continue;
-                    const double w = r.weight(s.exp2_table, v[j]);
-                    const int b = r.bin(v[j]);
-                    all += w;
-                    if (b < b1) above += w;
-                    else if (b <= b2) atomicAdd(&s.mass[b], __double2ull_rn(w * kMassOne));
-                }
-            });
-            t = r.template add_up<false>(all, above, 0, 0.f, 0);
-            const double target = pd * t.sum[0] * kMassOne;
-            r.merge_hist(true);                             // (the counts again: they have not changed)
-            r.find_mass(t.sum[1] * kMassOne, target);
-            if (s.found[3] != 0) {
-                const int b = s.found[0], in = s.found[2];
-                const double mass0 = s.found_mass;
-                __syncthreads();
-                cut = r.template cut_in_group<true>(
-                    [&](float x, u64 o) { return inside(x, index_of(o)) && r.bin(x) == b; }, in, 0, mass0, target);
-            } else if (target <= 0.0) {
-                cut = order_of(r.top, (1 << kIndexBits) - 1);                 // p = 0: the largest value
+            const bool listed = k <= kMaxTopLogits && ahead + in <= 4096;
+            if (!listed) cut = r.template cut_in_group<false>(data([&](float x, int) { return x > -INFINITY && r.bin(x) == b; }), k - ahead, 0.0, 0.0);
+            if (k <= kMaxTopLogits) {
+                log_full = log(r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0]);
+                const int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
+                if (r.rank != 0) return;
+                return draw_from_list(r, r.sort_top(n, k), p, m, u, write);
             }
             cut_value = value_of(cut);
             cut_index = index_of(cut);
         }
-        // The kept entries: those in the bins below b1 have been added up.  min-p takes its entries one by one.
-        const double m_from = by_m ? static_cast<double>(r.top) + log(md) / r.inv_t : 0.0;
-        const float m_floor = by_m ? static_cast<float>(m_from - 1e-6 * (fabs(static_cast<double>(r.top)) + fabs(m_from)) - 1e-30) : -INFINITY;
-        if (by_m) {
-            b1 = 0;
-            above = 0.0;
-        }
-        const float c = static_cast<float>(1.4426950408889634 * r.inv_t);
-        const bool sum_full = !by_k && !by_p;
-        r.each([&](const float (&v)[kEach], int i, int) {
-            float f = 0.f;
+        double above = 0.0;                                       // kept mass (this thread's part)
+        bool counted = false;                                     // kept holds the entries that `above` and the lists sum up
+        if (threadIdx.x < kSelWarps) s.warp_listed[threadIdx.x] = 0;
+        if (by_p) {
+            if (by_k) {                                           // the histogram of what top-k has left
+                __syncthreads();
+                r.clear_hist();
+                r.template each<kDeep>([&](const float (&v)[kEach], int i, int) {
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                if (sum_full) f += ex2_approx((v[j] - r.top) * c);
-                if (v[j] < m_floor || !inside(v[j], i + j)) continue;
-                if (r.bin(v[j]) >= b1) {
+                    for (int j = 0; j < kEach; ++j)
+                        if (inside(v[j], i + j)) atomicAdd(&s.hist[r.bin(v[j])], 1u);
+                });
+                r.merge_hist();
+            }
+            // the cut lies in none of the bins before b1 and none behind b2
+            int b1, b2;
+            r.bracket(pd, 0.0, 0.0, 0, b1, b2);
+            const int before = s.found[0];
+            __syncthreads();
+            // one pass for the total and for the mass before b1
+            const float from_bin = kTwo23 + b1;
+            double all = 0.0;
+            auto add = [&](auto limited) {
+                r.template each<2>([&](const float (&v)[kEach], int i, int) {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) {
+                        bool in = v[j] >= r.weight.floor;
+                        if constexpr (decltype(limited)::value) in = in && inside(v[j], i + j);
+                        const double w = r.weight.of(s.exp2_table, fmaxf(v[j], r.weight.floor));
+                        if (in) all += w;
+                        if (in && r.bin_f(v[j]) < from_bin) above += w;
+                    }
+                });
+            };
+            if (by_k) add(std::true_type());
+            else add(std::false_type());
+            t = r.template add_up<false>(all, above, 0, 0.f, 0);
+            if (!by_k) full = all;                                // (there is no fp32 sum)
+            const double target = pd * t.sum[0], mass_b1 = t.sum[1];
+            if (target <= 0.0) {
+                cut = order_of(r.top, (1 << kIndexBits) - 1);     // p = 0: the largest value
+            } else {
+                // with the two sums the counts say more: the cut is in none of the bins behind c2
+                int c1, c2;
+                r.bracket(pd, t.sum[0], mass_b1, b1, c1, c2);
+                const int between = s.found[0] + s.found[1] - before;
+                const float to_bin = kTwo23 + min(b2, c2);
+                auto open = [&](float x, int i) {
+                    const float bf = r.bin_f(x);
+                    return bf >= from_bin && bf <= to_bin && x > -INFINITY && inside(x, i);
+                };
+                __syncthreads();
+                if (between <= 2 * kListCap) {
+                    // every CTA lists its entries from b1 on
+                    if (threadIdx.x == 0) s.list_n = 0;
+                    __syncthreads();
+                    data(open)([&](float, u64 o) { s.indices[atomicAdd(&s.list_n, 1)] = index_of(o); });
+                    __syncthreads();
+                    const int n = s.list_n;
+                    auto listed = [&](auto f) {
+#pragma unroll 4
+                        for (int i = threadIdx.x; i < n; i += kSelThreads) {
+                            const int at = s.indices[i];
+                            const float x = to_f32(r.x[at]);
+                            f(x, order_of(x, at));
+                        }
+                    };
+                    cut = r.template cut_in_group<true>(
+                        listed,
+                        0, mass_b1 * kMassOne, target * kMassOne);
+                    if (!by_m) {
+                        counted = true;
+                        listed([&](float x, u64 o) {
+                            if (o > cut) return;
+                            add_u64(&s.warp_listed[r.warp_of(index_of(o))], r.mass(x));
+                            ++kept;
+                        });
+                        if (r.rank == 0 && threadIdx.x == 0) kept += before;
+                    }
+                } else {
+                    cut = r.template cut_in_group<true>(data(open), 0, mass_b1 * kMassOne, target * kMassOne);
+                }
+            }
+            cut_value = value_of(cut);
+            cut_index = index_of(cut);
+        }
+        if (!counted) {
+            above = 0.0;
+            const double m_from = by_m ? static_cast<double>(r.top) + log(md) / r.inv_t : 0.0;
+            const float m_floor = by_m ? static_cast<float>(m_from - 1e-6 * (fabs(static_cast<double>(r.top)) + fabs(m_from)) - 1e-30) : -INFINITY;
+            const float c = static_cast<float>(1.4426950408889634 * r.inv_t);
+            const bool sum_full = !by_k && !by_p;
+            r.template each<2>([&](const float (&v)[kEach], int i, int) {
+                float f = 0.f;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    if (sum_full) f += ex2_approx((v[j] - r.top) * c);
+                    if (!(v[j] >= m_floor) || !inside(v[j], i + j)) continue;
                     const double w = r.weight(s.exp2_table, v[j]);
                     if (by_m && w < md && v[j] != r.top) continue;
                     above += w;
+                    ++kept;
                 }
-                ++kept;
-            }
-            if (sum_full) full += static_cast<double>(f);
-        });
-        const double of_warp = warp_sum(above);
+                if (sum_full) full += static_cast<double>(f);
+            });
+        }
+        __syncthreads();
+        const double of_warp = warp_sum(above) + static_cast<double>(s.warp_listed[warp]) / kMassOne;
         if (lane == 0) s.warp_kept[warp] = of_warp;
-        t = r.template add_up<false>(above, full, kept, 0.f, 0);
+        t = r.template add_up<false>(lane == 0 ? of_warp : 0.0, full, kept, 0.f, 0);
         log_full = log(t.sum[1]);
         kept = t.count;
         if (by_p && p == 0.f) {                                   // ties of the largest value: the first of them alone
@@ -1222,11 +1315,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
 
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid_constant__ SelectArgs a) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    SelShared& s = *reinterpret_cast<SelShared*>(smem);
+    SelShared& s = smem();
     pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
-    Row<T> r(s, a, row, static_cast<int>(blockIdx.x % a.cluster));
+    Row<T> r(a, row, static_cast<int>(blockIdx.x % a.cluster));
     auto write = [&](int n, float lse) {                          // n entries of the list, and padding
         for (int i = threadIdx.x; i < a.K; i += kSelThreads) {
             a.ids[row * a.ld_out + i] = i < n ? index_of(s.list[i]) : -1;
@@ -1241,7 +1333,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
     };
     if (a.mask && a.mask[row] == 0) return neutral(0u, 0.f);
     r.inv_t = 1.0 / static_cast<double>(a.tau);
-    if (a.K * r.C <= kListCap) {
+    if (a.K * r.C <= 4096) {
         float about;
         double full;
         const int n = r.stream_top(a.K, r.inv_t, about, full);
@@ -1255,26 +1347,34 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
     if (t.bad) return neutral(AIS_FLAG_NONFINITE, NAN);
     if (t.top == -INFINITY) return neutral(AIS_FLAG_EMPTY, -INFINITY);
     r.set_scale(t.top, r.inv_t);
-    const double full = r.template add_up<false>(r.histogram(), 0.0, 0, 0.f, 0).sum[0];
+    const double full = r.template add_up<false>(r.template histogram<true>(), 0.0, 0, 0.f, 0).sum[0];
     const int k = min(a.K, t.count);
-    r.find_count(k);
+    r.template find_count<kBins>(r.counts(), k);
     const int b = s.found[0], ahead = s.found[1], in = s.found[2];
     __syncthreads();
-    int n;
-    if (ahead + in <= kListCap) {
-        n = r.gather_sorted([&](float x, u64) { return x > -INFINITY && r.bin(x) <= b; });
-    } else {
-        const u64 cut = r.template cut_in_group<false>([&](float x, u64) { return x > -INFINITY && r.bin(x) == b; }, in, k - ahead, 0.0, 0.0);
-        n = r.gather_sorted([&](float, u64 o) { return o <= cut; });
-    }
+    const bool listed = ahead + in <= 4096;
+    u64 cut = 0;
+    if (!listed)
+        cut = r.template cut_in_group<false>(
+            [&](auto f) {
+                r.template each<kDeep>([&](const float (&v)[Row<T>::kEach], int i, int) {
+#pragma unroll
+                    for (int j = 0; j < Row<T>::kEach; ++j)
+                        if (v[j] > -INFINITY && r.bin(v[j]) == b) f(v[j], order_of(v[j], i + j));
+                });
+            },
+            k - ahead, 0.0, 0.0);
+    int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
+    if (r.rank == 0) n = r.sort_top(n, k);
     if (r.rank == 0) write(min(n, k), static_cast<float>(static_cast<double>(r.top) * r.inv_t + log(full)));
 }
 
 template <typename K>
 cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream) {
-    // More CTAs per row while the rows alone do not fill two CTAs per SM, and a slice keeps 16 KB.
+    // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  (Not beyond: the cluster's barriers and the
+    // merging cost more than a better filled last wave gives; 613 rows of 151936 bf16, K = 64: one CTA 109 us, four 349.)
     int c = 1;
-    while (c < kMaxCluster && rows * c < 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
+    while (c < kMaxCluster && rows * c * 2 <= 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
     a.cluster = c;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rows * c));
