@@ -316,8 +316,7 @@ struct Row {
     // The entries before the first and behind the last whole chunk, fewer than kEach each, belong to the first warp of the first CTA
     // (before its chunks) and to the last warp of the last CTA (behind its chunks).  One of them as a chunk filled up with -inf at its end;
     // false if there is none (for this warp).
-    __device__ __forceinline__ bool edge(bool tail, float (&v)[kEach], int& i) const {
-        const int warp = threadIdx.x >> 5;
+    __device__ __forceinline__ bool edge(bool tail, int warp, float (&v)[kEach], int& i) const {
         int n;
         if (tail) {
             i = first_index(whole);
@@ -331,9 +330,9 @@ struct Row {
         return n > 0;
     }
     // A warp owns consecutive chunks of the slice.
-    __device__ __forceinline__ void range(int& from, int& to) const {
+    __device__ __forceinline__ void range(int warp, int& from, int& to) const {
         const int per = ((c1 - c0 + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
-        from = min(c0 + static_cast<int>(threadIdx.x >> 5) * per, c1);
+        from = min(c0 + warp * per, c1);
         to = min(from + per, c1);
     }
     // f(values, index of the first, how many are part of the row) for everything this warp owns, a thread at a time, B chunks of it in flight.
@@ -342,7 +341,7 @@ struct Row {
     template <int B, typename F>
     __device__ __forceinline__ void each(F f) const {
         int from, to;
-        range(from, to);
+        range(threadIdx.x >> 5, from, to);
         const int lane = threadIdx.x & 31;
         uint4 raw[B];
 #pragma unroll
@@ -361,7 +360,7 @@ struct Row {
         if (lane < 2) {
             float v[kEach];
             int i;
-            if (edge(lane == 1, v, i)) f(v, i, lane == 1 ? V - i : head);
+            if (edge(lane == 1, threadIdx.x >> 5, v, i)) f(v, i, lane == 1 ? V - i : head);
         }
     }
 
@@ -374,6 +373,17 @@ struct Row {
     // The histogram bin of a value as a float above 2^23, whose low bits are the bin: the distance below the maximum in bins, rounded.
     __device__ __forceinline__ float bin_f(float v) const { return fminf(fmaf(top - v, bins, kTwo23), kTwo23 + (kBins - 1)); }
     __device__ __forceinline__ int bin(float v) const { return static_cast<int>(__float_as_uint(bin_f(v)) & (kBins - 1)); }
+    // The largest value whose bin is `b` or a later one (bin_f falls as its value rises): a comparison with it does for one with the bin.
+    __device__ float edge_value(int b) const {
+        uint32_t lo = 0x007fffffu, hi = 0xff800000u;              // -inf and +inf in ascending order (order_of() before it is turned over)
+        while (hi - lo > 1u) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const float v = __uint_as_float(mid ^ ((mid >> 31) != 0u ? 0x80000000u : 0xffffffffu));
+            if (v > top || bin_f(v) < kTwo23 + b) hi = mid;
+            else lo = mid;
+        }
+        return __uint_as_float(lo ^ ((lo >> 31) != 0u ? 0x80000000u : 0xffffffffu));
+    }
     __device__ __forceinline__ u64 mass(float v) const { return __double2ull_rn(weight(smem().exp2_table, v) * kMassOne); }
     __device__ __forceinline__ const uint32_t* counts() const { return C > 1 ? smem().tot : smem().hist; }
     __device__ __forceinline__ const uint32_t* parts() const { return C > 1 ? smem().part_tot : smem().part; }
@@ -868,7 +878,7 @@ struct Row {
         auto ends = [&](bool tail, float above) {                 // the entries outside the whole chunks
             float v[kEach], f = 0.f;
             int i;
-            if ((threadIdx.x & 31) != 0 || !edge(tail, v, i)) return;
+            if ((threadIdx.x & 31) != 0 || !edge(tail, threadIdx.x >> 5, v, i)) return;
             push(v, i, above);
 #pragma unroll
             for (int k = 0; k < kEach; ++k) f += ex2_approx((v[k] - ref) * c);
@@ -1139,7 +1149,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
             const int before = s.found[0];
             __syncthreads();
             // one pass for the total and for the mass before b1
-            const float from_bin = kTwo23 + b1;
+            const float from_value = r.edge_value(b1);            // values above it lie in the bins before b1
             double all = 0.0;
             auto add = [&](auto limited) {
                 r.template each<2>([&](const float (&v)[kEach], int i, int) {
@@ -1149,7 +1159,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
                         if constexpr (decltype(limited)::value) in = in && inside(v[j], i + j);
                         const double w = r.weight.of(s.exp2_table, fmaxf(v[j], r.weight.floor));
                         if (in) all += w;
-                        if (in && r.bin_f(v[j]) < from_bin) above += w;
+                        if (in && v[j] > from_value) above += w;
                     }
                 });
             };
@@ -1165,11 +1175,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
                 int c1, c2;
                 r.bracket(pd, t.sum[0], mass_b1, b1, c1, c2);
                 const int between = s.found[0] + s.found[1] - before;
-                const float to_bin = kTwo23 + min(b2, c2);
-                auto open = [&](float x, int i) {
-                    const float bf = r.bin_f(x);
-                    return bf >= from_bin && bf <= to_bin && x > -INFINITY && inside(x, i);
-                };
+                const float to_value = min(b2, c2) < kBins - 1 ? r.edge_value(min(b2, c2) + 1) : -INFINITY;
+                auto open = [&](float x, int i) { return x <= from_value && x > to_value && (!by_k || inside(x, i)); };
                 __syncthreads();
                 if (between <= 2 * kListCap) {
                     // every CTA lists its entries from b1 on
@@ -1236,81 +1243,101 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
             t.sum[0] = 1.0;
         }
     }
-    // The token: the CTA, the warp and the entry at which the kept mass exceeds u times its total.  Sums of the same terms in another
-    // order may differ in their last bits, so the last candidate of each step takes what is left.
+    // The token: the CTA, the warp's range, a sixteenth of that and the entry at which the kept mass exceeds u times its total.  Sums of
+    // the same terms in another order may differ in their last bits, so the last candidate of each step takes what is left.
     const bool first_only = by_p && p == 0.f;
     const double want = first_only ? 0.0 : ud * t.sum[0];
-    // (t.before of the next CTA is this one's t.before + mine, the same sum: one CTA takes it)
+    constexpr double kNone = 1e-290;                              // (entries of -inf may add up to a little less than that)
+    auto choose = [&](const double* sums, double left) {          // one thread
+        int chosen = -1;
+        double ahead = 0.0;
+        for (int w = 0; w < kSelWarps; ++w) {
+            if (sums[w] <= kNone) continue;
+            chosen = w;
+            s.found_mass = left - ahead;
+            if (left - ahead < sums[w]) break;
+            ahead += sums[w];
+        }
+        s.found[0] = chosen;
+    };
     if (threadIdx.x == 0) {
         double mine = 0.0;
-        const double before = want - t.before;
-        int chosen = -1;
         for (int w = 0; w < kSelWarps; ++w) mine += s.warp_kept[w];
         s.found[0] = -1;
-        if (want >= t.before && mine > 0.0 && want < t.before + mine) {
-            double ahead = 0.0;
-            for (int w = 0; w < kSelWarps; ++w) {
-                if (s.warp_kept[w] <= 0.0) continue;
-                chosen = w;
-                s.found_mass = before - ahead;
-                if (before - ahead < s.warp_kept[w]) break;
-                ahead += s.warp_kept[w];
-            }
-            s.found[0] = chosen;
-        }
+        // (t.before of the next CTA is this one's t.before + mine, the same sum: one CTA takes it)
+        if (want >= t.before && mine > kNone && want < t.before + mine) choose(s.warp_kept, want - t.before);
     }
     __syncthreads();
-    if (s.found[0] != warp) return;
+    const int owner = s.found[0];
+    if (owner < 0) return;
+    double left = s.found_mass;
     const float cut_value = value_of(cut), m_top = r.top;
     const int cut_index = index_of(cut);
-    double left = s.found_mass;
     int from, to;
-    u64 last = ~0ull;                                             // the last entry with a mass (per lane)
-    r.range(from, to);
-    for (int base = from - 32; base < to + 32; base += 32) {      // the head of the row, the chunks, its tail
-        float v[kEach];
-        double w[kEach], sum = 0.0;
-        int i;
-        if (base < from || base >= to) {
-            if (!r.edge(base >= to, v, i)) continue;
+    r.range(owner, from, to);
+    // the chunks of the range in steps of 32, its head and tail as steps of their own; the weights of a step
+    const int steps = (to - from + 31) / 32 + 2, share = (steps + kSelWarps - 1) / kSelWarps;
+    auto step = [&](int n, float (&v)[kEach], int& i, double (&w)[kEach]) {
+        if (n == 0 || n == steps - 1) {
+            r.edge(n != 0, owner, v, i);
             if (lane > 0) {
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) v[j] = -INFINITY;
             }
         } else {
-            Elem<T>::unpack(r.chunk(base + lane, to), v);
-            i = r.first_index(base + lane);
+            const int c = from + (n - 1) * 32 + lane;
+            Elem<T>::unpack(r.chunk(c, to), v);
+            i = r.first_index(c);
         }
+        double sum = 0.0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const bool in = v[j] > cut_value || (v[j] == cut_value && i + j <= cut_index);
             w[j] = in ? r.weight(s.exp2_table, v[j]) : 0.0;
             if (by_m && w[j] < md && v[j] != m_top) w[j] = 0.0;
             sum += w[j];
-            if (w[j] > 0.0) last = order_of(v[j], i + j);
         }
+        return sum;
+    };
+    const int n0 = warp * share, n1 = min(n0 + share, steps);
+    float v[kEach];
+    double w[kEach], sum = 0.0;
+    int i;
+    for (int n = n0; n < n1; ++n) sum += step(n, v, i, w);
+    sum = warp_sum(sum);
+    __syncthreads();
+    if (lane == 0) s.warp_f64[0][warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) choose(s.warp_f64[0], left);
+    __syncthreads();
+    if (s.found[0] != warp) return;
+    left = s.found_mass;
+    u64 last = ~0ull;                                             // the last entry with a mass (per lane)
+    for (int n = n0; n < n1; ++n) {
+        sum = step(n, v, i, w);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (w[j] > 0.0) last = order_of(v[j], i + j);
         const double inc = warp_scan(sum);
         const unsigned hit = __ballot_sync(0xffffffffu, inc > left);
         if (hit) {
             if (lane == __ffs(hit) - 1) {
-                double at = inc - sum;
-                u64 o = last;
+                double c = inc - sum;
+                u64 o = ~0ull;
 #pragma unroll
-                for (int j = kEach - 1; j >= 0; --j) {            // the first whose sum exceeds what is left
-                    double c = at;
-                    for (int q = 0; q <= j; ++q) c += w[q];
-                    if (w[j] > 0.0 && c > left) o = order_of(v[j], i + j);
+                for (int j = 0; j < kEach; ++j) {                 // the first whose sum exceeds what is left
+                    c += w[j];
+                    if (o == ~0ull && w[j] > 0.0 && c > left) o = order_of(v[j], i + j);
                 }
-                write(o, log(t.sum[0]), kept);
+                write(o == ~0ull ? last : o, log(t.sum[0]), kept);
             }
             return;
         }
         left -= __shfl_sync(0xffffffffu, inc, 31);
     }
-    // (rounding: the warp's last entry; the later index is the later lane's or chunk's)
-    int index = last == ~0ull ? -1 : index_of(last);
-    const int largest = __reduce_max_sync(0xffffffffu, index);
-    if (index == largest && index >= 0) write(last, log(t.sum[0]), kept);
+    // (rounding: the last entry of all; a later step is a later index, and so is a later lane)
+    const int index = last == ~0ull ? -1 : index_of(last);
+    if (index == __reduce_max_sync(0xffffffffu, index) && index >= 0) write(last, log(t.sum[0]), kept);
 }
 
 template <typename T>
