@@ -110,6 +110,8 @@ struct SelectArgs {
     int64_t ld;
     int V;
     int cluster;
+    int rows_of;             // sampling: kAllRows, or one of the two kinds
+    int late;                // nothing of the kernel before is needed: it is waited for at the end only
     const uint8_t* mask;
     uint32_t* status;
     // sampling
@@ -126,6 +128,9 @@ struct SelectArgs {
     float* lse;
     int64_t ld_out;
 };
+
+// Rows of one pass (few large entries, or no filter at all), and rows that need several.
+enum { kAllRows = 0, kOnePass = 1, kManyPasses = 2 };
 
 // 0 (the largest entry) or at least AIS_MIN_TEMPERATURE; not NaN, not infinite.
 __host__ __device__ inline bool usable_temperature(float t) { return t == 0.f || (t >= AIS_MIN_TEMPERATURE && t < INFINITY); }
@@ -771,33 +776,30 @@ struct Row {
         bins = static_cast<float>(kBinsPerNat * inv_t_);
         weight.set(inv_t, static_cast<double>(top_));
     }
+    // This chunk's part in the row's maximum (NaN if there is one) and in the number of its entries of -inf.
+    static __device__ __forceinline__ void see(const float (&v)[kEach], int n, float& most, int& missing) {
+        float least = v[0];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            most = max_nan(most, v[k]);
+            least = fminf(least, v[k]);
+        }
+        if (least == -INFINITY) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) missing += k < n && v[k] == -INFINITY;
+        }
+    }
     // The row's maximum, number of finite entries and whether it holds a NaN or +inf.
     __device__ Totals look() const {
-        float m = -INFINITY, least = INFINITY;
-        each<kDeep>([&](const float (&v)[kEach], int, int n) {
-#pragma unroll
-            for (int k = 0; k < kEach; ++k) {
-                m = max_nan(m, v[k]);
-                least = fminf(least, k < n ? v[k] : INFINITY);
-            }
-        });
-        return extremes(0.0, m, least);
+        float most = -INFINITY;
+        int missing = 0;
+        each<kDeep>([&](const float (&v)[kEach], int, int n) { see(v, n, most, missing); });
+        return extremes(0.0, most, missing);
     }
-    // Totals of a pass that has seen this thread's maximum (NaN if there was one) and minimum.  Entries of -inf are counted only where
-    // there are any.
-    __device__ Totals extremes(double sum, float m, float least) const {
-        Totals t = add_up<true>(sum, 0.0, 0, isnan(m) ? -INFINITY : m, (m < INFINITY ? 0 : 1) | (least == -INFINITY ? 2 : 0));
-        if ((t.bad & 2) != 0) {
-            int finite = 0;
-            each<kDeep>([&](const float (&v)[kEach], int, int) {
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) finite += v[k] > -INFINITY;
-            });
-            t.count = add_up<false>(0.0, 0.0, finite, 0.f, 0).count;
-        } else {
-            t.count = V;
-        }
-        t.bad &= 1;
+    // Totals of a pass that has seen all of this thread's chunks.
+    __device__ Totals extremes(double sum, float most, int missing) const {
+        Totals t = add_up<true>(sum, 0.0, missing, isnan(most) ? -INFINITY : most, most < INFINITY ? 0 : 1);
+        t.count = V - t.count;
         return t;
     }
     // Histogram of the row, merged; with SUM also the fp32 sum of its exponentials about `top` (this thread's part).
@@ -875,13 +877,15 @@ struct Row {
                 }
             return at;
         };
+        // 2^(v c + shift) with one multiply-add; the rounding of shift (and that of c, for values near ref) is taken back at the end
+        const float shift = -ref * c;
         auto ends = [&](bool tail, float above) {                 // the entries outside the whole chunks
             float v[kEach], f = 0.f;
             int i;
             if ((threadIdx.x & 31) != 0 || !edge(tail, threadIdx.x >> 5, v, i)) return;
             push(v, i, above);
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) f += ex2_approx((v[k] - ref) * c);
+            for (int k = 0; k < kEach; ++k) f += ex2_approx(fmaf(v[k], c, shift));
             full += static_cast<double>(f);
         };
         ends(false, thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY);
@@ -902,7 +906,7 @@ struct Row {
                 for (int k = 1; k < kEach; ++k) m = fmaxf(m, v[k]);
                 if (m > above) pushed = push(v, first_index(c0 + t0 + j * kSelThreads + threadIdx.x), above);
 #pragma unroll
-                for (int k = 0; k < kEach; ++k) f += ex2_approx((v[k] - ref) * c);
+                for (int k = 0; k < kEach; ++k) f += ex2_approx(fmaf(v[k], c, shift));
             }
             full += static_cast<double>(f);
             if (t0 + kTile >= n) break;
@@ -918,6 +922,7 @@ struct Row {
             }
         }
         ends(true, thr);
+        full *= exp2(-(static_cast<double>(ref) * static_cast<double>(c) + static_cast<double>(shift)));
         __syncthreads();
         overflow |= s.list_n > 4096;
         if (C == 1) return overflow ? -1 : sort_top(s.list_n, K);
@@ -945,6 +950,9 @@ struct Row {
         return rank != 0 ? 0 : sort_top(all, K);
     }
 };
+
+// Is a row with these parameters done in one pass (but for what one pass finds to be too much)?
+__host__ __device__ inline bool one_pass(int k, float p, float m) { return k > 0 ? k <= kMaxTopLogits : p >= 1.f && !(m > 0.f); }
 
 // The first min(k, n) entries of the sorted list in rank 0: masses ahead of every entry give top-p, the value min-p; then the token by
 // the masses in the order of the indices.
@@ -986,9 +994,8 @@ __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Writ
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_constant__ SelectArgs a) {
+__device__ __forceinline__ void sample_row(const SelectArgs& a) {
     SelShared& s = smem();
-    pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
     Row<T> r(a, row, static_cast<int>(blockIdx.x % a.cluster));
     constexpr int kEach = Row<T>::kEach;
@@ -1000,18 +1007,20 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         if (a.n_kept) a.n_kept[row] = 0;
         if (flag && a.status) atomicOr(a.status, flag);
     };
-    if (a.mask && a.mask[row] == 0) return neutral(0u);
+    const bool first_kind = a.rows_of != kManyPasses;             // (rows that give nothing are of the first)
+    if (a.mask && a.mask[row] == 0) return first_kind ? neutral(0u) : void();
     float temperature = a.how.temperature_rows ? a.how.temperature_rows[row] : a.how.temperature;
     int k = a.how.top_k_rows ? a.how.top_k_rows[row] : a.how.top_k;
     const float p = a.how.top_p_rows ? a.how.top_p_rows[row] : a.how.top_p;
     const float m = a.how.min_p_rows ? a.how.min_p_rows[row] : a.how.min_p;
     const float u = a.u[row];
     // (each comparison is false for a NaN)
-    if (!usable_temperature(temperature) || !(p >= 0.f) || !(m <= 1.f) || !(u >= 0.f && u < 1.f)) return neutral(AIS_FLAG_PARAM);
+    if (!usable_temperature(temperature) || !(p >= 0.f) || !(m <= 1.f) || !(u >= 0.f && u < 1.f)) return first_kind ? neutral(AIS_FLAG_PARAM) : void();
     if (temperature == 0.f) {
         temperature = 1.f;
         k = 1;
     }
+    if (a.rows_of != kAllRows && one_pass(k, p, m) != first_kind) return;
     {
         const double e = exp2((threadIdx.x >> 3) / 64.0);
         static_assert(kSelThreads == 64 * 8 && kTableCopies == 16, "eight threads write the copies of an entry");
@@ -1054,32 +1063,19 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
         for (int again = 0;; ++again) {
             r.weight.set(r.inv_t, about_d);
             double sum = 0.0;
-            float top = -INFINITY, least = INFINITY;
-            r.template each<2>([&](const float (&v)[kEach], int i, int n) {
-                float mn = v[0];
+            float most = -INFINITY;
+            int missing = 0;
+            r.template each<2>([&](const float (&v)[kEach], int, int n) {
+                r.see(v, n, most, missing);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
-                    top = max_nan(top, v[j]);
-                    mn = fminf(mn, v[j]);
-                }
-                if (n == kEach) least = fminf(least, mn);
-                if (mn >= r.weight.floor) {
-#pragma unroll
-                    for (int j = 0; j < kEach; ++j) sum += r.weight.of(s.exp2_table, v[j]);
-                } else {
-                    for (int j = 0; j < n; ++j) least = fminf(least, to_f32(r.x[i + j]));
-#pragma unroll 1
-                    for (int j = 0; j < kEach; ++j) {
-                        float x = v[0];
-#pragma unroll
-                        for (int q = 1; q < kEach; ++q) x = q == j ? v[q] : x;
-                        sum += r.weight(s.exp2_table, x);
-                    }
+                    const double w = r.weight.of(s.exp2_table, fmaxf(v[j], r.weight.floor));
+                    if (v[j] >= r.weight.floor) sum += w;
                 }
             });
             const double of_warp = warp_sum(sum);
             if (lane == 0) s.warp_kept[warp] = of_warp;
-            t = r.extremes(sum, top, least);
+            t = r.extremes(sum, most, missing);
             if (again || t.bad || t.top == -INFINITY || fabs(t.top * r.inv_t) < 600.0) break;
             about_d = t.top;
         }
@@ -1341,6 +1337,14 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
 }
 
 template <typename T>
+__global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_constant__ SelectArgs a) {
+    if (!a.late) pdl_wait();
+    pdl_trigger();
+    sample_row<T>(a);
+    if (a.late) pdl_wait();
+}
+
+template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid_constant__ SelectArgs a) {
     SelShared& s = smem();
     pdl_enter();
@@ -1397,11 +1401,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
 }
 
 template <typename K>
-cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream) {
+cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream, int forced = 0) {
     // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  (Not beyond: the cluster's barriers and the
     // merging cost more than a better filled last wave gives; 613 rows of 151936 bf16, K = 64: one CTA 109 us, four 349.)
     int c = 1;
     while (c < kMaxCluster && rows * c * 2 <= 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
+    if (forced > 0)
+        for (c = 1; c < forced && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384; c *= 2) {}
     a.cluster = c;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rows * c));
@@ -1480,9 +1486,21 @@ int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t l
     a.lp_full = lp_full;
     a.n_kept = n_kept;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = dtype == AIS_BF16  ? launch_select(sample_kernel<__nv_bfloat16>, a, rows, 2, s)
-                          : dtype == AIS_F16 ? launch_select(sample_kernel<__half>, a, rows, 2, s)
-                                             : launch_select(sample_kernel<float>, a, rows, 4, s);
+    auto launch = [&](int forced) {
+        return dtype == AIS_BF16  ? launch_select(sample_kernel<__nv_bfloat16>, a, rows, 2, s, forced)
+               : dtype == AIS_F16 ? launch_select(sample_kernel<__half>, a, rows, 2, s, forced)
+                                  : launch_select(sample_kernel<float>, a, rows, 4, s, forced);
+    };
+    // Rows with filters of their own: the few that need several passes get four CTAs each, in a launch of their own that the others overlap
+    // (256 x 151936 bf16 with mixed parameters: one launch 207 us, two MIXED_US).
+    cudaError_t e = cudaSuccess;
+    if (how->top_k_rows || how->top_p_rows || how->min_p_rows) {
+        a.rows_of = kManyPasses;
+        e = launch(4);
+        a.rows_of = kOnePass;
+        a.late = 1;
+    }
+    if (e == cudaSuccess) e = launch(0);
     return e == cudaSuccess ? AIS_OK : AIS_ERR_DEVICE;
 }
 
