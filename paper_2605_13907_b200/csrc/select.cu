@@ -50,7 +50,8 @@ constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight
 constexpr int kBins = 8192;
 constexpr int kListCap = 4096;           // entries of a list
 constexpr int kSplit = 1024;             // ways in which a group of entries is divided
-constexpr int kListPrune = 2048;         // a list is cut back beyond this
+constexpr int kListPrune = 3072;         // a list is cut back beyond this
+constexpr int kFew = 256;                // entries of a group that are not divided any more
 constexpr int kRankSort = 256;           // entries up to which a list is sorted by counting
 constexpr int kMaxCluster = 8;
 constexpr float kBinsPerNat = 256.f;
@@ -84,6 +85,8 @@ struct alignas(16) SelShared {
             u64 mass_tot[kSplit];
             uint32_t part[kSplit];
             uint32_t part_tot[kSplit];
+            u64 few[kFew];               // the last entries of a group
+            u64 few_mass[kFew];
         };
         struct {
             uint32_t small_hist[kSelThreads];
@@ -93,13 +96,13 @@ struct alignas(16) SelShared {
     double exp2_table[64 * kTableCopies];   // 2^(j / 64)
     double warp_kept[kSelWarps];         // kept mass of every warp's range
     u64 warp_listed[kSelWarps];          // what the list adds to it
-    Published pub;
+    Published pub[2];                    // in turn, so that one barrier per exchange is enough
     double warp_f64[2][kSelWarps];
     u64 warp_u64[2][kSelWarps];
     int warp_int[kSelWarps];
     double found_mass;
     int found[4];
-    int list_n;
+    int list_n, list_few;
 };
 // (through the array itself and not through a pointer in a struct: the compiler then knows that it is shared memory)
 extern __shared__ __align__(16) unsigned char select_smem[];
@@ -304,6 +307,7 @@ struct Row {
     float bins;              // histogram bins per unit of x
     double inv_t;
     Weight weight;           // about `top`
+    mutable int turn = 0;    // which of the two pub[] the next exchange uses
 
     __device__ Row(const SelectArgs& a, int64_t row, int rank_) : V(a.V), C(a.cluster), rank(rank_) {
         x = static_cast<const T*>(a.x) + row * a.ld;
@@ -454,22 +458,22 @@ struct Row {
                     bad |= static_cast<int>(s.warp_u64[0][w] >> 32);
                 }
             }
-            s.pub.sum[0] = a;
-            s.pub.sum[1] = b;
-            s.pub.count = n;
-            if (MAX) { s.pub.top = top_; s.pub.bad = bad; }
+            s.pub[turn].sum[0] = a;
+            s.pub[turn].sum[1] = b;
+            s.pub[turn].count = n;
+            if (MAX) { s.pub[turn].top = top_; s.pub[turn].bad = bad; }
         }
         sync();
         Totals t = {{0.0, 0.0}, 0.0, -INFINITY, 0, 0};
         for (int r = 0; r < C; ++r) {
-            const Published* p = remote(&s.pub, r);
+            const Published* p = remote(&s.pub[turn], r);
             if (r == rank) t.before = t.sum[0];
             t.sum[0] += p->sum[0];
             t.sum[1] += p->sum[1];
             t.count += p->count;
             if (MAX) { t.top = fmaxf(t.top, p->top); t.bad |= p->bad; }
         }
-        sync();
+        turn ^= 1;
         return t;
     }
     // The first of n counts, n a multiple of the threads, at which their sum reaches k (k >= 1, no more than the total): s.found = {which,
@@ -520,47 +524,55 @@ struct Row {
     // From the merged counts: the bins b1 .. b2 in which the mass can reach the target.  An entry of bin b weighs between e^(-(b + 1/2) / 256)
     // and e^(-(b - 1/2) / 256), but for the rounding of the bin (1e-6 of a distance of 32) and of the exponentials here: 2e-5 to either side.
     // Without a total the target is p times the sum, which is bounded alike; with it, bins before b0 weigh `mass0` together.
-    // s.found = {entries before b1, entries from b1 to b2}.
-    __device__ void bracket(double p, double total, double mass0, int from, int& b1, int& b2) const {
+    // s.found = {entries before b1, entries from b1 to b2, b1, b2}.  (Apart: its registers would be taken from the passes around it.)
+    static __device__ __noinline__ void bracket(bool one, double p, double total, double mass0, int from) {
         SelShared& s = smem();
         constexpr int kMine = kBins / kSelThreads;
         const int b0 = threadIdx.x * kMine;
-        const uint32_t* count = counts();
         const float step = -1.4426950408889634f / kBinsPerNat;
+        uint32_t count[kMine];
+#pragma unroll
+        for (int j = 0; j < kMine; j += 4) *reinterpret_cast<uint4*>(count + j) = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0)[j / 4];
+        auto hi_of = [&](int j) { return static_cast<double>(static_cast<float>(count[j]) * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f)); };
+        auto lo_of = [&](int j) {
+            return b0 + j == kBins - 1 ? 0.0 : static_cast<double>(static_cast<float>(count[j]) * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
+        };
         double hs = 0.0, ls = 0.0, h_total, l_total;
-        for (int j = 0; j < kMine; ++j) {
-            const float c = static_cast<float>(count[b0 + j]);    // (exact below 2^24)
-            if (c == 0.f || b0 + j < from) continue;
-            hs += static_cast<double>(c * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f));
-            ls += b0 + j == kBins - 1 ? 0.0 : static_cast<double>(c * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
-        }
-        double h = mass0 + block_scan(hs, s.warp_f64[0], h_total);
-        double l = mass0 + block_scan(ls, s.warp_f64[0], l_total);
-        const double to_lo = p * (total > 0.0 ? total : l_total), to_hi = p * (total > 0.0 ? total : h_total);
-        int n1 = 0, n2 = 0;
-        for (int j = 0; j < kMine; ++j) {
-            const float c = static_cast<float>(count[b0 + j]);
-            if (c != 0.f && b0 + j >= from) {
-                h += static_cast<double>(c * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f));
-                l += b0 + j == kBins - 1 ? 0.0 : static_cast<double>(c * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+            if (b0 + j >= from) {
+                hs += hi_of(j);
+                ls += lo_of(j);
             }
-            n1 += b0 + j < from || h < to_lo;
-            n2 += b0 + j < from || l < to_hi;
-        }
-        block_scan(n1, s.warp_int, b1);
-        b1 = min(b1, kBins - 1);
-        block_scan(n2, s.warp_int, b2);
-        b2 = min(b2, kBins - 1);
-        int before = 0, in = 0, sum;
+        double h = mass0 + block_scan(hs, s.warp_f64[0], h_total);
+        double l = mass0 + block_scan(ls, s.warp_f64[1], l_total);
+        const double to_lo = p * (total > 0.0 ? total : l_total), to_hi = p * (total > 0.0 ? total : h_total);
+        int n = 0;                                                // bins before b1, and (times 2^16) those before b2 + 1
+#pragma unroll
         for (int j = 0; j < kMine; ++j) {
-            const int c = static_cast<int>(count[b0 + j]);
-            if (b0 + j < b1) before += c;
-            else if (b0 + j <= b2) in += c;
+            if (b0 + j >= from) {
+                h += hi_of(j);
+                l += lo_of(j);
+            }
+            n += (b0 + j < from || h < to_lo ? 1 : 0) + (b0 + j < from || l < to_hi ? 1 << 16 : 0);
         }
-        block_scan(before, s.warp_int, sum);
-        if (threadIdx.x == 0) s.found[0] = sum;
-        block_scan(in, s.warp_int, sum);
-        if (threadIdx.x == 0) s.found[1] = sum;
+        int sum;
+        block_scan(n, s.warp_int, sum);
+        const int b1 = min(sum & 0xffff, kBins - 1), b2 = min(sum >> 16, kBins - 1);
+        u64 entries = 0;                                          // before b1, and (times 2^32) from b1 to b2
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+            if (b0 + j < b1) entries += count[j];
+            else if (b0 + j <= b2) entries += static_cast<u64>(count[j]) << 32;
+        }
+        u64 all;
+        block_scan(entries, s.warp_u64[0], all);
+        if (threadIdx.x == 0) {
+            s.found[0] = static_cast<int>(all & 0xffffffffu);
+            s.found[1] = static_cast<int>(all >> 32);
+            s.found[2] = b1;
+            s.found[3] = b2;
+        }
         __syncthreads();
     }
     // Entries that keep(value, index) takes, 4,096 at most, go to the list of rank 0; only rank 0 has it (and its length).
@@ -700,16 +712,19 @@ struct Row {
         return min(sort_list(n), K);
     }
     // The cut inside a group of `count` entries, those that over(f) calls f(value, number) for, in all CTAs: by count, the entry number `want`
-    // (from 1) of the group; by mass, the first at which mass0 plus the masses reach `target` (in units of 2^-44).  The range of numbers is
-    // divided 1,024 ways, and again the part with the cut, until one number is left; by mass, the last of the group where rounding
-    // leaves none.  No list is touched.
+    // (from 1) of the group; by mass, the first at which mass0 plus the masses reach `target` (in units of 2^-44), and the last of the
+    // group where rounding leaves none.  The range of numbers is divided 1,024 ways, and again the part with the cut, until no more
+    // than 256 entries are left; they go to rank 0, where each adds up those before it.
     template <bool MASS, typename Over>
-    __device__ u64 cut_in_group(Over over, int want, double mass0, double target) const {
+    __device__ u64 cut_in_group(Over over, int count, int want, double mass0, double target) const {
         SelShared& s = smem();
-        u64 lo = ~0ull, hi = 0;
-        over([&](float, u64 o) { lo = min(lo, o); hi = max(hi, o); });
-        for (;;) {
-            // what is left of the group, its ends
+        u64 from = 0, to = ~0ull;
+        while (count > kFew) {
+            // the ends of what is left of the group
+            u64 lo = ~0ull, hi = 0;
+            over([&](float, u64 o) {
+                if (o >= from && o <= to) { lo = min(lo, o); hi = max(hi, o); }
+            });
             for (int o = 16; o > 0; o >>= 1) {
                 lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
                 hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
@@ -723,19 +738,16 @@ struct Row {
             __syncthreads();
             if (threadIdx.x == 0) {
                 for (int w = 0; w < kSelWarps; ++w) { lo = min(lo, s.warp_u64[0][w]); hi = max(hi, s.warp_u64[1][w]); }
-                s.pub.lo = lo;
-                s.pub.hi = hi;
+                s.pub[turn].lo = lo;
+                s.pub[turn].hi = hi;
             }
             sync();
             for (int r = 0; r < C; ++r) {
-                lo = min(lo, remote(&s.pub, r)->lo);
-                hi = max(hi, remote(&s.pub, r)->hi);
+                lo = min(lo, remote(&s.pub[turn], r)->lo);
+                hi = max(hi, remote(&s.pub[turn], r)->hi);
             }
-            if (lo >= hi) {                                       // one number, or (a group without entries) none
-                sync();
-                return hi;
-            }
-            const int bits = 64 - __clzll(hi - lo);
+            turn ^= 1;
+            const int bits = 64 - __clzll(hi - lo);               // (more than 256 numbers: hi > lo)
             const int shift = bits > 10 ? bits - 10 : 0;
             over([&](float x, u64 o) {
                 if (o < lo || o > hi) return;
@@ -757,17 +769,46 @@ struct Row {
                 find_count<kSplit>(parts(), want);
                 want -= s.found[1];
             }
-            const u64 from = lo + (static_cast<u64>(s.found[0]) << shift), to = min(hi, from + ((1ull << shift) - 1));
-            if (shift == 0) {
-                sync();
-                return from;
-            }
-            lo = ~0ull;
-            hi = 0;
-            over([&](float, u64 o) {
-                if (o >= from && o <= to) { lo = min(lo, o); hi = max(hi, o); }
-            });
+            count = s.found[2];
+            from = lo + (static_cast<u64>(s.found[0]) << shift);
+            to = min(hi, from + ((1ull << shift) - 1));
         }
+        sync();                                                   // (nobody reads the parts of rank 0 any more)
+        if (threadIdx.x == 0) s.list_few = 0;
+        sync();
+        int* counter = remote(&s.list_few, 0);
+        u64* few = remote(s.few, 0);
+        over([&](float, u64 o) {
+            if (o < from || o > to) return;
+            const int at = atomicAdd(counter, 1);
+            if (at < kFew) few[at] = o;
+        });
+        sync();
+        if (rank == 0) {
+            const int n = min(s.list_few, kFew);
+            const u64 o = threadIdx.x < n ? s.few[threadIdx.x] : 0;
+            const u64 m = MASS && threadIdx.x < n ? mass(value_of(o)) : 1;
+            if (threadIdx.x < n) s.few_mass[threadIdx.x] = m;
+            if (threadIdx.x == 0) s.pub[turn].lo = n > 0 ? 0 : last_finite();
+            __syncthreads();
+            if (threadIdx.x < n) {
+                u64 before = 0;
+                bool is_last = true;
+                for (int i = 0; i < n; ++i) {
+                    const u64 other = s.few[i];
+                    if (other < o) before += s.few_mass[i];
+                    else if (other > o) is_last = false;
+                }
+                const double lo = mass0 + static_cast<double>(before), hi = mass0 + static_cast<double>(before + m);
+                const bool cut = MASS ? (lo < target && hi >= target) || (is_last && hi < target) : before + 1 == static_cast<u64>(want);
+                if (cut) s.pub[turn].lo = o;
+            }
+            __syncthreads();
+        }
+        sync();
+        const u64 cut = remote(&s.pub[turn], 0)->lo;
+        turn ^= 1;
+        return cut;
     }
 
     __device__ void set_scale(float top_, double inv_t_) {
@@ -889,7 +930,7 @@ struct Row {
             full += static_cast<double>(f);
         };
         ends(false, thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY);
-        int tile = 0, limit = max(512, 4 * K);
+        int tile = 0, limit = min(max(512, 4 * K), kListPrune);
 #pragma unroll 1
         for (int t0 = 0; t0 < n; t0 += kTile, ++tile) {
             int pushed = 0;
@@ -928,19 +969,20 @@ struct Row {
         if (C == 1) return overflow ? -1 : sort_top(s.list_n, K);
         // the K largest of every slice, sorted together by rank 0
         const int mine = overflow ? -1 : sort_top(s.list_n, K);
-        if (threadIdx.x == 0) { s.pub.count = mine; s.pub.top = ref; }
+        if (threadIdx.x == 0) { s.pub[turn].count = mine; s.pub[turn].top = ref; }
         sync();
         int at = 0, all = 0;
         for (int r = 0; r < C; ++r) {
-            const int k = remote(&s.pub, r)->count;
+            const int k = remote(&s.pub[turn], r)->count;
             if (k < 0) overflow = true;
             if (r < rank) at += k;
             all += k;
         }
         // every CTA's sum about the reference of rank 0
-        const float ref0 = remote(&s.pub, 0)->top;
+        const float ref0 = remote(&s.pub[turn], 0)->top;
         full *= exp2(static_cast<double>((ref - ref0) * c));
         ref = ref0;
+        turn ^= 1;
         if (!overflow && rank != 0) {
             u64* list = remote(s.list, 0) + at;
             for (int i = threadIdx.x; i < mine; i += kSelThreads) list[i] = s.list[i];
@@ -991,6 +1033,11 @@ __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Writ
             if (index_of(s.list[j]) < v) c += w_of[j];
         if (c <= t && t < c + w_of[i]) write(s.list[i], log(static_cast<double>(total) / kMassOne), n_kept);
     }
+}
+
+// The end of a row, by every thread: no CTA leaves while another of its cluster may still read what it has published.
+__device__ __forceinline__ void leave_row(int cluster) {
+    if (cluster > 1) cg::this_cluster().sync();
 }
 
 template <typename T>
@@ -1115,7 +1162,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             const int b = s.found[0], ahead = s.found[1], in = s.found[2];
             __syncthreads();
             const bool listed = k <= kMaxTopLogits && ahead + in <= 4096;
-            if (!listed) cut = r.template cut_in_group<false>(data([&](float x, int) { return x > -INFINITY && r.bin(x) == b; }), k - ahead, 0.0, 0.0);
+            if (!listed) cut = r.template cut_in_group<false>(data([&](float x, int) { return x > -INFINITY && r.bin(x) == b; }), in, k - ahead, 0.0, 0.0);
             if (k <= kMaxTopLogits) {
                 log_full = log(r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0]);
                 const int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
@@ -1140,9 +1187,8 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                 r.merge_hist();
             }
             // the cut lies in none of the bins before b1 and none behind b2
-            int b1, b2;
-            r.bracket(pd, 0.0, 0.0, 0, b1, b2);
-            const int before = s.found[0];
+            r.bracket(r.C == 1, pd, 0.0, 0.0, 0);
+            const int before = s.found[0], b1 = s.found[2], b2 = s.found[3];
             __syncthreads();
             // one pass for the total and for the mass before b1
             const float from_value = r.edge_value(b1);            // values above it lie in the bins before b1
@@ -1168,9 +1214,8 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                 cut = order_of(r.top, (1 << kIndexBits) - 1);     // p = 0: the largest value
             } else {
                 // with the two sums the counts say more: the cut is in none of the bins behind c2
-                int c1, c2;
-                r.bracket(pd, t.sum[0], mass_b1, b1, c1, c2);
-                const int between = s.found[0] + s.found[1] - before;
+                r.bracket(r.C == 1, pd, t.sum[0], mass_b1, b1);
+                const int c2 = s.found[3], between = s.found[0] + s.found[1] - before;
                 const float to_value = min(b2, c2) < kBins - 1 ? r.edge_value(min(b2, c2) + 1) : -INFINITY;
                 auto open = [&](float x, int i) { return x <= from_value && x > to_value && (!by_k || inside(x, i)); };
                 __syncthreads();
@@ -1190,8 +1235,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                         }
                     };
                     cut = r.template cut_in_group<true>(
-                        listed,
-                        0, mass_b1 * kMassOne, target * kMassOne);
+                        listed, between, 0, mass_b1 * kMassOne, target * kMassOne);
                     if (!by_m) {
                         counted = true;
                         listed([&](float x, u64 o) {
@@ -1202,7 +1246,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                         if (r.rank == 0 && threadIdx.x == 0) kept += before;
                     }
                 } else {
-                    cut = r.template cut_in_group<true>(data(open), 0, mass_b1 * kMassOne, target * kMassOne);
+                    cut = r.template cut_in_group<true>(data(open), between, 0, mass_b1 * kMassOne, target * kMassOne);
                 }
             }
             cut_value = value_of(cut);
@@ -1341,13 +1385,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) sample_kernel(const __grid_con
     if (!a.late) pdl_wait();
     pdl_trigger();
     sample_row<T>(a);
+    leave_row(a.cluster);
     if (a.late) pdl_wait();
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid_constant__ SelectArgs a) {
+__device__ __forceinline__ void top_row(const SelectArgs& a) {
     SelShared& s = smem();
-    pdl_enter();
     const int64_t row = blockIdx.x / a.cluster;
     Row<T> r(a, row, static_cast<int>(blockIdx.x % a.cluster));
     auto write = [&](int n, float lse) {                          // n entries of the list, and padding
@@ -1394,10 +1438,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
                         if (v[j] > -INFINITY && r.bin(v[j]) == b) f(v[j], order_of(v[j], i + j));
                 });
             },
-            k - ahead, 0.0, 0.0);
+            in, k - ahead, 0.0, 0.0);
     int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
     if (r.rank == 0) n = r.sort_top(n, k);
     if (r.rank == 0) write(min(n, k), static_cast<float>(static_cast<double>(r.top) * r.inv_t + log(full)));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid_constant__ SelectArgs a) {
+    pdl_enter();
+    top_row<T>(a);
+    leave_row(a.cluster);
 }
 
 template <typename K>
