@@ -522,7 +522,7 @@ struct Row {
         __syncthreads();
     }
     // From the merged counts: the bins b1 .. b2 in which the mass can reach the target.  An entry of bin b weighs between e^(-(b + 1/2) / 256)
-    // and e^(-(b - 1/2) / 256), but for the rounding of the bin (1e-6 of a distance of 32) and of the exponentials here: 2e-5 to either side.
+    // and e^(-(b - 1/2) / 256), but for the rounding of the bin (4e-6) and of the sums here (6e-6): 2e-5 to either side.
     // Without a total the target is p times the sum, which is bounded alike; with it, bins before b0 weigh `mass0` together.
     // s.found = {entries before b1, entries from b1 to b2, b1, b2}.  (Apart: its registers would be taken from the passes around it.)
     static __device__ __noinline__ void bracket(bool one, double p, double total, double mass0, int from) {
@@ -533,29 +533,29 @@ struct Row {
         uint32_t count[kMine];
 #pragma unroll
         for (int j = 0; j < kMine; j += 4) *reinterpret_cast<uint4*>(count + j) = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0)[j / 4];
-        auto hi_of = [&](int j) { return static_cast<double>(static_cast<float>(count[j]) * (ex2_approx((b0 + j - 0.5f) * step) * 1.00002f)); };
-        auto lo_of = [&](int j) {
-            return b0 + j == kBins - 1 ? 0.0 : static_cast<double>(static_cast<float>(count[j]) * (ex2_approx((b0 + j + 0.5f) * step) * 0.99998f));
-        };
-        double hs = 0.0, ls = 0.0, h_total, l_total;
+        // the exponentials of the bins by steps of e^(-1/256) from the thread's first; a thread's sums in fp32 (3e-6 relative, like the steps)
+        const float down = 0.99610137f, first = ex2_approx((b0 - 0.5f) * step);
+        auto walk = [&](auto f) {
+            float e = first, hs = 0.f, ls = 0.f;
 #pragma unroll
-        for (int j = 0; j < kMine; ++j)
-            if (b0 + j >= from) {
-                hs += hi_of(j);
-                ls += lo_of(j);
+            for (int j = 0; j < kMine; ++j) {
+                const float c = b0 + j >= from ? static_cast<float>(count[j]) : 0.f;
+                hs = fmaf(c * 1.00002f, e, hs);
+                e *= down;
+                ls = fmaf(b0 + j < kBins - 1 ? c * 0.99998f : 0.f, e, ls);
+                f(hs, ls, j);
             }
-        double h = mass0 + block_scan(hs, s.warp_f64[0], h_total);
-        double l = mass0 + block_scan(ls, s.warp_f64[1], l_total);
+        };
+        float hs = 0.f, ls = 0.f;
+        walk([&](float h, float l, int) { hs = h; ls = l; });
+        double h_total, l_total;
+        const double h = mass0 + block_scan(static_cast<double>(hs), s.warp_f64[0], h_total);
+        const double l = mass0 + block_scan(static_cast<double>(ls), s.warp_f64[1], l_total);
         const double to_lo = p * (total > 0.0 ? total : l_total), to_hi = p * (total > 0.0 ? total : h_total);
         int n = 0;                                                // bins before b1, and (times 2^16) those before b2 + 1
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-            if (b0 + j >= from) {
-                h += hi_of(j);
-                l += lo_of(j);
-            }
-            n += (b0 + j < from || h < to_lo ? 1 : 0) + (b0 + j < from || l < to_hi ? 1 << 16 : 0);
-        }
+        walk([&](float hj, float lj, int j) {
+            n += (b0 + j < from || h + static_cast<double>(hj) < to_lo ? 1 : 0) + (b0 + j < from || l + static_cast<double>(lj) < to_hi ? 1 << 16 : 0);
+        });
         int sum;
         block_scan(n, s.warp_int, sum);
         const int b1 = min(sum & 0xffff, kBins - 1), b2 = min(sum >> 16, kBins - 1);
@@ -575,6 +575,24 @@ struct Row {
         }
         __syncthreads();
     }
+    // put(place, value, index) for the entries that keep(value, index) takes; places from *counter on, one atomic for those of a chunk (with
+    // one for each entry they queue up: 2,000 took 25 us).
+    template <typename F, typename G>
+    __device__ __forceinline__ void collect(F keep, int* counter, G put) const {
+        each<kDeep>([&](const float (&v)[kEach], int i, int) { collect_chunk(v, i, keep, counter, put); });
+    }
+    template <typename F, typename G>
+    static __device__ __forceinline__ int collect_chunk(const float (&v)[kEach], int i, F keep, int* counter, G put) {
+        unsigned taken = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) taken |= (keep(v[k], i + k) ? 1u : 0u) << k;
+        if (taken == 0u) return 0;
+        int at = atomicAdd(counter, __popc(taken));
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (taken >> k & 1u) put(at++, v[k], i + k);
+        return at;
+    }
     // Entries that keep(value, index) takes, 4,096 at most, go to the list of rank 0; only rank 0 has it (and its length).
     template <typename F>
     __device__ int gather(F keep) const {
@@ -582,19 +600,9 @@ struct Row {
         sync();                                    // the list shares its place with the counts
         if (threadIdx.x == 0) s.list_n = 0;
         sync();
-        int* counter = remote(&s.list_n, 0);
         u64* list = remote(s.list, 0);
-        each<kDeep>([&](const float (&v)[kEach], int i, int) {
-            unsigned taken = 0;
-#pragma unroll
-            for (int k = 0; k < kEach; ++k) taken |= (keep(v[k], i + k) ? 1u : 0u) << k;
-            if (taken == 0u) return;
-#pragma unroll
-            for (int k = 0; k < kEach; ++k)
-                if (taken >> k & 1u) {
-                    const int at = atomicAdd(counter, 1);
-                    if (at < kListCap) list[at] = order_of(v[k], i + k);
-                }
+        collect(keep, remote(&s.list_n, 0), [=](int at, float x, int i) {
+            if (at < kListCap) list[at] = order_of(x, i);
         });
         sync();
         return rank == 0 ? min(s.list_n, 4096) : 0;
@@ -909,14 +917,9 @@ struct Row {
             if (!(fabsf(ref) < INFINITY)) ref = 0.f;
         }
         auto push = [&](const float (&v)[kEach], int i, float above) {
-            int at = 0;
-#pragma unroll
-            for (int k = 0; k < kEach; ++k)
-                if (v[k] > above) {
-                    at = atomicAdd(&s.list_n, 1);
-                    if (at < kListCap) s.list[at] = order_of(v[k], i + k);
-                }
-            return at;
+            return collect_chunk(v, i, [=](float x, int) { return x > above; }, &s.list_n, [&](int at, float x, int index) {
+                if (at < kListCap) s.list[at] = order_of(x, index);
+            });
         };
         // 2^(v c + shift) with one multiply-add; the rounding of shift (and that of c, for values near ref) is taken back at the end
         const float shift = -ref * c;
@@ -1223,7 +1226,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                     // every CTA lists its entries from b1 on
                     if (threadIdx.x == 0) s.list_n = 0;
                     __syncthreads();
-                    data(open)([&](float, u64 o) { s.indices[atomicAdd(&s.list_n, 1)] = index_of(o); });
+                    r.collect(open, &s.list_n, [&](int at, float, int i) { s.indices[at] = i; });
                     __syncthreads();
                     const int n = s.list_n;
                     auto listed = [&](auto f) {
