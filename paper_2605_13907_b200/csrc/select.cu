@@ -50,7 +50,8 @@ constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight
 constexpr int kBins = 8192;
 constexpr int kListCap = 4096;           // entries of a list
 constexpr int kSplit = 1024;             // ways in which a group of entries is divided
-constexpr int kListPrune = 3072;         // a list is cut back beyond this
+constexpr int kChunkCap = 3072;          // chunks in the list of a pass for the largest entries
+constexpr int kChunkPrune = 2048;        // which is cut back beyond this
 constexpr int kFew = 256;                // entries of a group that are not divided any more
 constexpr int kRankSort = 256;           // entries up to which a list is sorted by counting
 constexpr int kMaxCluster = 8;
@@ -91,6 +92,7 @@ struct alignas(16) SelShared {
         struct {
             uint32_t small_hist[kSelThreads];
             float group_max[2 * kSelThreads];
+            u64 chunks[kChunkCap];       // 16-byte chunks with a large entry: that entry above, the chunk below
         };
     };
     double exp2_table[64 * kTableCopies];   // 2^(j / 64)
@@ -693,19 +695,28 @@ struct Row {
         }
         return lo;
     }
-    // The list without the entries below `thr`.
-    __device__ void drop_below(float thr, int n) const {
-        SelShared& s = smem();
-        constexpr int kMine = 4096 / kSelThreads;
-        u64 o[kMine];                                             // (n <= 4096)
+    static __device__ __forceinline__ float most_of(u64 chunk) { return __uint_as_float(static_cast<uint32_t>(chunk >> 32)); }
+    // The n entries of a list that keep(entry) takes, moved together; their number to *counter.
+    template <int CAP, typename F>
+    static __device__ void compact(u64* list, int n, int* counter, F keep) {
+        constexpr int kMine = CAP / kSelThreads;
+        u64 o[kMine];
+        unsigned taken = 0;
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) o[j] = threadIdx.x + j * kSelThreads < n ? s.list[threadIdx.x + j * kSelThreads] : ~0ull;
+        for (int j = 0; j < kMine; ++j) {
+            const int i = threadIdx.x + j * kSelThreads;
+            o[j] = i < n ? list[i] : 0;
+            taken |= (i < n && keep(o[j]) ? 1u : 0u) << j;
+        }
         __syncthreads();
-        if (threadIdx.x == 0) s.list_n = 0;
+        if (threadIdx.x == 0) *counter = 0;
         __syncthreads();
+        if (taken != 0u) {
+            int at = atomicAdd(counter, __popc(taken));
 #pragma unroll
-        for (int j = 0; j < kMine; ++j)
-            if (o[j] != ~0ull && value_of(o[j]) >= thr) s.list[atomicAdd(&s.list_n, 1)] = o[j];
+            for (int j = 0; j < kMine; ++j)
+                if (taken >> j & 1u) list[at++] = o[j];
+        }
         __syncthreads();
     }
     // The K largest of the first n entries of the list, sorted; returns their number.
@@ -713,7 +724,7 @@ struct Row {
         SelShared& s = smem();
         if (n > kRankSort && n > K + K / 4 + 8) {
             const float thr = bound([&](int i) { return value_of(s.list[i]); }, n, K);
-            drop_below(thr, n);
+            compact<kListCap>(s.list, n, &s.list_n, [=](u64 o) { return value_of(o) >= thr; });
             n = s.list_n;
             __syncthreads();
         }
@@ -872,14 +883,15 @@ struct Row {
     }
 
     // The K largest entries by one pass: rank 0 gets them sorted in s.list and returns their number, and the fp32 sum of exponentials
-    // about `ref` in `full` (all threads of all CTAs).  -1: the list overflowed, or the sum says that the row needs a closer look.
+    // about `ref` in `full` (all threads of all CTAs).  -1: a list overflowed, or the sum says that the row needs a closer look.
+    // What the pass lists is chunks, by their largest entry (a fifth of the instructions that the entries themselves would take: 592 x 151936
+    // bf16, K = 64, STREAM_US); the K-th of the K chunks listed first bounds the K-th entry from below as well.
     __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
         SelShared& s = smem();
         constexpr int kTile = kSelThreads * kDeep;
         const float c = static_cast<float>(1.4426950408889634 * inv_t_);
         const int n = c1 - c0;
-        float* group_max = s.group_max;
-        if (threadIdx.x == 0) s.list_n = 0;
+        if (threadIdx.x == 0) s.list_n = s.list_few = 0;
         __syncthreads();
         uint4 raw[kDeep];
         float thr = -INFINITY;
@@ -889,7 +901,7 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) raw[j] = chunk(c0 + j * kSelThreads + threadIdx.x, c1);
         if (n > 0) {
-            // groups: the entries of a thread's first and of its last loads, of a thread, or of two threads
+            // a bound from the first tile.  Groups: the entries of a thread's first and of its last loads, of a thread, or of two threads
             float half[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int j = 0; j < kDeep; ++j) {
@@ -902,44 +914,49 @@ struct Row {
             int groups;
             if (K > kSelThreads / 2) {
                 groups = 2 * kSelThreads;
-                group_max[2 * threadIdx.x] = half[0];
-                group_max[2 * threadIdx.x + 1] = half[1];
+                s.group_max[2 * threadIdx.x] = half[0];
+                s.group_max[2 * threadIdx.x + 1] = half[1];
             } else if (K > kSelThreads / 8) {
                 groups = kSelThreads;
-                group_max[threadIdx.x] = both;
+                s.group_max[threadIdx.x] = both;
             } else {
                 groups = kSelThreads / 2;
                 both = fmaxf(both, __shfl_xor_sync(0xffffffffu, both, 1));
-                if ((threadIdx.x & 1) == 0) group_max[threadIdx.x / 2] = both;
+                if ((threadIdx.x & 1) == 0) s.group_max[threadIdx.x / 2] = both;
             }
             __syncthreads();
-            thr = bound([&](int i) { return group_max[i]; }, groups, K, &ref);
+            thr = bound([&](int i) { return s.group_max[i]; }, groups, K, &ref);
             if (!(fabsf(ref) < INFINITY)) ref = 0.f;
         }
-        auto push = [&](const float (&v)[kEach], int i, float above) {
-            return collect_chunk(v, i, [=](float x, int) { return x > above; }, &s.list_n, [&](int at, float x, int index) {
-                if (at < kListCap) s.list[at] = order_of(x, index);
-            });
+        // a chunk whose largest entry is above `above`: its place in the list
+        auto push = [&](float most, int at_chunk) {
+            const int at = atomicAdd(&s.list_n, 1);
+            if (at < kChunkCap) s.chunks[at] = (static_cast<u64>(__float_as_uint(most)) << 32) | static_cast<uint32_t>(at_chunk);
+            return at;
         };
         // 2^(v c + shift) with one multiply-add; the rounding of shift (and that of c, for values near ref) is taken back at the end
         const float shift = -ref * c;
-        auto ends = [&](bool tail, float above) {                 // the entries outside the whole chunks
-            float v[kEach], f = 0.f;
+        auto ends = [&](bool tail, float above) {                 // the entries outside the whole chunks: chunk -1, chunk `whole`
+            float v[kEach], f = 0.f, m = -INFINITY;
             int i;
             if ((threadIdx.x & 31) != 0 || !edge(tail, threadIdx.x >> 5, v, i)) return;
-            push(v, i, above);
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) f += ex2_approx(fmaf(v[k], c, shift));
+            for (int k = 0; k < kEach; ++k) {
+                m = fmaxf(m, v[k]);
+                f += ex2_approx(fmaf(v[k], c, shift));
+            }
+            if (m > above) push(m, tail ? whole : -1);
             full += static_cast<double>(f);
         };
-        ends(false, thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY);
-        int tile = 0, limit = min(max(512, 4 * K), kListPrune);
+        // (>= in the first tile, whose entries gave the bound; later ones of the same value come after K entries in the order)
+        const float first_above = thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY;
+        ends(false, first_above);
+        int tile = 0, limit = min(max(512, 4 * K), kChunkPrune);
 #pragma unroll 1
         for (int t0 = 0; t0 < n; t0 += kTile, ++tile) {
             int pushed = 0;
             float f = 0.f;
-            // (>= in the first tile, whose entries gave the bound; later ones of the same value come after K entries in the order)
-            const float above = tile == 0 ? nextafterf(thr, -INFINITY) : thr;
+            const float above = tile == 0 ? first_above : thr;
 #pragma unroll
             for (int j = 0; j < kDeep; ++j) {
                 float v[kEach];
@@ -948,7 +965,7 @@ struct Row {
                 float m = v[0];
 #pragma unroll
                 for (int k = 1; k < kEach; ++k) m = fmaxf(m, v[k]);
-                if (m > above) pushed = push(v, first_index(c0 + t0 + j * kSelThreads + threadIdx.x), above);
+                if (m > above) pushed = push(m, c0 + t0 + j * kSelThreads + threadIdx.x);
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) f += ex2_approx(fmaf(v[k], c, shift));
             }
@@ -957,21 +974,47 @@ struct Row {
             // a tighter bound each time the list has doubled
             if (__syncthreads_or(pushed >= limit)) {
                 const int have = s.list_n;                        // (nobody adds to it here)
-                if (have > 4096) { overflow = true; break; }
+                if (have > kChunkCap) { overflow = true; break; }
                 __syncthreads();
-                if (have > K) thr = fmaxf(thr, bound([&](int i) { return value_of(s.list[i]); }, have, K));
-                if (have > kListPrune) drop_below(thr, have);
-                limit = min(2 * s.list_n, kListPrune);
+                if (have > K) thr = fmaxf(thr, bound([&](int i) { return most_of(s.chunks[i]); }, have, K));
+                if (have > kChunkPrune) compact<kChunkCap>(s.chunks, have, &s.list_n, [=](u64 o) { return most_of(o) >= thr; });
+                limit = min(2 * s.list_n, kChunkPrune);
                 __syncthreads();
             }
         }
         ends(true, thr);
         full *= exp2(-(static_cast<double>(ref) * static_cast<double>(c) + static_cast<double>(shift)));
         __syncthreads();
-        overflow |= s.list_n > 4096;
-        if (C == 1) return overflow ? -1 : sort_top(s.list_n, K);
+        const int listed = s.list_n;
+        overflow |= listed > kChunkCap;
+        if (!overflow) {
+            // the entries of the listed chunks that reach the last bound
+            if (listed > K) thr = fmaxf(thr, bound([&](int i) { return most_of(s.chunks[i]); }, listed, K));
+            for (int q = threadIdx.x; q < listed; q += kSelThreads) {
+                const u64 entry = s.chunks[q];
+                if (most_of(entry) < thr) continue;
+                const int at_chunk = static_cast<int>(static_cast<uint32_t>(entry));
+                float v[kEach];
+                int i = 0;
+                if (at_chunk >= 0 && at_chunk < whole) {
+                    Elem<T>::unpack(chunk(at_chunk, whole), v);
+                    i = first_index(at_chunk);
+                } else {
+                    const int m = at_chunk < 0 ? head : V;        // where these entries end
+                    if (at_chunk >= 0) i = first_index(whole);
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) v[k] = i + k < m ? to_f32(x[i + k]) : -INFINITY;
+                }
+                collect_chunk(v, i, [=](float value, int) { return value >= thr && value > -INFINITY; }, &s.list_few, [&](int at, float value, int index) {
+                    if (at < kListCap) s.list[at] = order_of(value, index);
+                });
+            }
+            __syncthreads();
+            overflow = s.list_few > kListCap;
+        }
+        const int mine = overflow ? -1 : sort_top(s.list_few, K);
+        if (C == 1) return mine;
         // the K largest of every slice, sorted together by rank 0
-        const int mine = overflow ? -1 : sort_top(s.list_n, K);
         if (threadIdx.x == 0) { s.pub[turn].count = mine; s.pub[turn].top = ref; }
         sync();
         int at = 0, all = 0;
