@@ -1196,6 +1196,7 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
     job.scale = keep ? reinterpret_cast<float*>(ws + L.off_scale) : nullptr;
     job.U = keep ? U : nullptr;
     job.ldU = L.ldU;
+    job.redo = grads != 0;
     job.redo_flags = ws + L.off_redo;
     job.redo_count = counters + 1;
     job.partials = reinterpret_cast<double*>(ws + L.off_partials);
@@ -1232,7 +1233,7 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
         a.part_z = a.part_s + L.part_bytes / sizeof(float);
         a.U = U;
         a.ldU = L.ldU;
-        a.keep_rows = keep ? rows : 0;
+        a.keep_rows = grads != 0 ? rows : 0;
         a.x_scale = static_cast<float>(job.inv_tau * (1.0 + kTruncationPerStep * (shape->d / 16)));
         a.picks = K;
         a.pick_ids = sorted_ids;
@@ -1246,7 +1247,8 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
             ++pass;
             return plan.two ? launch_lmhead_pair(mode, tmH, tmW_k, tail_map, a, ctas, s) : launch_lmhead(mode, tmH, tmW_k, tail_map, tmW_k, a, ctas, s);
         };
-        if (logits_pass(keep ? (dv ? kFwdPickKeepDv : kFwdPickKeep) : dv ? kFwdPickDv : kFwdPick) != cudaSuccess) return AIS_ERR_DEVICE;
+        const int mode = keep ? (dv ? kFwdPickKeepDv : kFwdPickKeep) : dW ? (dv ? kFwdPickCodeDv : kFwdPickCode) : dv ? kFwdPickDv : kFwdPick;
+        if (logits_pass(mode) != cudaSuccess) return AIS_ERR_DEVICE;
         job.row0 = r0;
         job.rows = rows;
         job.part_m = a.part_m;
@@ -1255,14 +1257,14 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
         job.part_ld = a.part_ld;
         if (launch_distill_rows(job, s) != cudaSuccess) return AIS_ERR_DEVICE;
         if (grads == 0) continue;
-        // the scratch in plain form (for dW), or only the rows that the exponent form does not reach (a gate that is usually closed)
+        // for dW the scratch in its final scale; then, behind a gate that is usually closed, the rows that neither form reaches
+        if (dW && launch_expand({U, L.ldU, rows, shape->V, K, job.coef + r0, job.row_lse + r0, sorted_ids + r0 * K, pick + r0 * K}, s) != cudaSuccess)
+            return AIS_ERR_DEVICE;
         a.lse = job.row_lse;
         a.coef = job.coef;
         a.row_scale = job.scale;
-        if (keep) {
-            a.tile_active = ws + L.off_redo;
-            a.gate = job.redo_count;
-        }
+        a.tile_active = ws + L.off_redo;
+        a.gate = job.redo_count;
         if (logits_pass(dv ? kBwdPPickDv : kBwdPPick) != cudaSuccess) return AIS_ERR_DEVICE;
         if (dH) {
             a.dH = static_cast<__nv_bfloat16*>(dH);

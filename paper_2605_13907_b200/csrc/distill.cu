@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                 // the row's factor, and what the scratch holds at the listed columns: (p - r) e^lse, or coef (p - r)
                 if (a.scale) scale = kept ? static_cast<float>(w * mass * a.inv_tau * exp(-lse)) : 1.f;
                 const double f = kept ? exp(lse) : w * mass * a.inv_tau;
-                if (a.scale && !kept && coef != 0.f && lane == 0) {
+                if (a.redo && !exp_form(lse_out) && coef != 0.f && lane == 0) {
                     a.redo_flags[t / kBM] = 1;
                     atomicAdd(a.redo_count, 1u);
                 }
@@ -194,6 +194,51 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
     }
 }
 
+// A block has 8,192 columns of a row, 16 bytes of codes per thread and load.
+constexpr int kExpandCols = 8192;
+__global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ ExpandJob a) {
+    pdl_enter();
+    const int64_t t = blockIdx.y;
+    const int from = blockIdx.x * kExpandCols, to = min(from + kExpandCols, a.V);
+    uint4* row = reinterpret_cast<uint4*>(a.U + t * a.ldU);
+    const float coef = a.coef[t];
+    constexpr float kLog2e = 1.4426950408889634f;
+    const float step = kLog2e / kCodeSteps, shift = -(kCodeZero + a.lse[t]) * kLog2e;
+    uint4 raw[kExpandCols / 2048];
+    if (coef != 0.f) {
+#pragma unroll
+        for (int j = 0; j < kExpandCols / 2048; ++j) {
+            const int c = from + (j * 256 + threadIdx.x) * 8;
+            if (c < to) raw[j] = __ldcs(row + c / 8);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kExpandCols / 2048; ++j) {
+        const int c = from + (j * 256 + threadIdx.x) * 8;
+        if (c >= to) break;
+        uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = w[k] & 0xffffu, hi = w[k] >> 16;
+            const float x = lo != 0u && coef != 0.f ? coef * exp2f(fmaf(static_cast<float>(lo), step, shift)) : 0.f;
+            const float y = hi != 0u && coef != 0.f ? coef * exp2f(fmaf(static_cast<float>(hi), step, shift)) : 0.f;
+            const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
+            w[k] = *reinterpret_cast<const uint32_t*>(&p);
+        }
+        row[c / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    if (coef == 0.f) return;
+    __syncthreads();
+    const int32_t* ids = a.ids + t * a.K;
+    int lo = 0, hi = a.K;                                         // the first listed column of this block
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ids[mid] < from) lo = mid + 1;
+        else hi = mid;
+    }
+    for (int k = lo + threadIdx.x; k < a.K && ids[k] < to; k += 256) a.U[t * a.ldU + ids[k]] = __float2bfloat16(a.pick[t * a.K + k]);
+}
+
 __global__ void __launch_bounds__(256) live_rows_kernel(const __nv_bfloat16* src, int64_t ld, int d, const float* coef, __nv_bfloat16* dst) {
     pdl_enter();
     const int64_t t = blockIdx.x;
@@ -203,6 +248,22 @@ __global__ void __launch_bounds__(256) live_rows_kernel(const __nv_bfloat16* src
 }
 
 }  // namespace
+
+cudaError_t launch_expand(const ExpandJob& job, cudaStream_t stream) {
+    // (65,535 rows per launch at most: the y dimension of a grid)
+    for (int64_t r0 = 0; r0 < job.rows; r0 += 65535) {
+        ExpandJob part = job;
+        part.U += r0 * job.ldU;
+        part.rows = job.rows - r0 < 65535 ? job.rows - r0 : 65535;
+        part.coef += r0;
+        part.lse += r0;
+        part.ids += r0 * job.K;
+        part.pick += r0 * job.K;
+        const cudaError_t e = launch_pdl(expand_kernel, dim3((job.V + kExpandCols - 1) / kExpandCols, static_cast<unsigned>(part.rows)), 256, 0, stream, part);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
 
 cudaError_t launch_live_rows(const __nv_bfloat16* src, int64_t ld, int64_t rows, int32_t d, const float* coef, __nv_bfloat16* dst, cudaStream_t stream) {
     return launch_pdl(live_rows_kernel, static_cast<unsigned>(rows), 256, 0, stream, src, ld, d, coef, dst);

@@ -45,7 +45,8 @@ struct DistillJob {
     float* scale;              // [T] factor of the row in the dH pass; NULL: the scratch is in plain form everywhere
     __nv_bfloat16* U;          // scratch of this launch's rows in exponent form (with scale), else NULL
     int64_t ldU;
-    uint8_t* redo_flags;       // per row tile of the batch, zeroed before (with scale)
+    bool redo;                 // row tiles with a row outside exp_form are marked (with scale, and with codes in the scratch)
+    uint8_t* redo_flags;       // per row tile of the batch, zeroed before
     uint32_t* redo_count;
     double* partials;          // [ceil(T / kDistillRows)]
     int32_t n_partials;        // of the whole batch
@@ -55,6 +56,18 @@ struct DistillJob {
 };
 constexpr int kDistillRows = 8;         // rows of a block (a warp each)
 cudaError_t launch_distill_rows(const DistillJob& job, cudaStream_t stream);
+
+// Scratch rows of codes (logit_code in lmhead.cuh) to coef e^(x - lse), and what pick holds at the listed columns; zeros for rows with coef 0.
+// All per-row arrays begin at the first row of the scratch.
+struct ExpandJob {
+    __nv_bfloat16* U;
+    int64_t ldU, rows;
+    int32_t V, K;
+    const float *coef, *lse;
+    const int32_t* ids;
+    const float* pick;
+};
+cudaError_t launch_expand(const ExpandJob& job, cudaStream_t stream);
 
 // dst = src for the rows with coef != 0, zeros for the others; both with row stride ld.
 cudaError_t launch_live_rows(const __nv_bfloat16* src, int64_t ld, int64_t rows, int32_t d, const float* coef, __nv_bfloat16* dst, cudaStream_t stream);

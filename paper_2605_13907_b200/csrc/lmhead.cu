@@ -504,6 +504,8 @@ cudaError_t launch_lmhead(int mode, const CUtensorMap& tmA, const CUtensorMap& t
         case kFwdPickKeepDv: return launch_mode<kFwdPickKeepDv>(tmA, tmB, tmSA, args, num_ctas, stream);
         case kBwdPPick: return launch_mode<kBwdPPick>(tmA, tmB, tmSA, args, num_ctas, stream);
         case kBwdPPickDv: return launch_mode<kBwdPPickDv>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPickCode: return launch_mode<kFwdPickCode>(tmA, tmB, tmSA, args, num_ctas, stream);
+        case kFwdPickCodeDv: return launch_mode<kFwdPickCodeDv>(tmA, tmB, tmSA, args, num_ctas, stream);
     }
     return cudaErrorInvalidValue;
 }
@@ -518,7 +520,8 @@ cudaError_t lmhead_prepare() {
                                prepare_mode<kFwdFp8T>(), prepare_mode<kFwdMx>(), prepare_mode<kFwdMx4>(),
                                prepare_mode<kFwdBf16Dv>(), prepare_mode<kBwdPDv>(), prepare_mode<kBwdDhDv>(), prepare_mode<kFwdKeep>(),
                                prepare_mode<kFwdKeepDv>(), prepare_mode<kFwdPick>(), prepare_mode<kFwdPickDv>(), prepare_mode<kFwdPickKeep>(),
-                               prepare_mode<kFwdPickKeepDv>(), prepare_mode<kBwdPPick>(), prepare_mode<kBwdPPickDv>()};
+                               prepare_mode<kFwdPickKeepDv>(), prepare_mode<kBwdPPick>(), prepare_mode<kBwdPPickDv>(),
+                               prepare_mode<kFwdPickCode>(), prepare_mode<kFwdPickCodeDv>()};
     for (const cudaError_t e : all)
         if (e != cudaSuccess) return e;
     return cudaSuccess;

@@ -33,24 +33,28 @@ enum LmheadMode : int {
     kFwdPickKeepDv = 16,
     kBwdPPick      = 17,
     kBwdPPickDv    = 18,
+    // the forward pass that also leaves 16-bit codes of the scaled logits in the scratch (logit_code)
+    kFwdPickCode   = 19,
+    kFwdPickCodeDv = 20,
     // the dW pass with a bf16 result
-    kBwdDwHalf     = 19
+    kBwdDwHalf     = 21
 };
 
 // What a mode computes (its epilogue and work-unit shape), whatever the layout of W.
 __host__ __device__ constexpr int base_mode(int mode) {
-    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv || (mode >= kFwdPick && mode <= kFwdPickKeepDv) ? kFwdBf16
+    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv || (mode >= kFwdPick && mode <= kFwdPickKeepDv) || mode == kFwdPickCode || mode == kFwdPickCodeDv ? kFwdBf16
            : mode == kBwdPDv || mode == kBwdPPick || mode == kBwdPPickDv                                                ? kBwdP
            : mode == kBwdDhDv                                                                                           ? kBwdDh
            : mode == kBwdDwHalf                                                                                         ? kBwdDw
                                                                                                                         : mode;
 }
 // The passes of the distillation.
-__host__ __device__ constexpr bool pick_mode(int mode) { return mode >= kFwdPick && mode <= kBwdPPickDv; }
+__host__ __device__ constexpr bool pick_mode(int mode) { return mode >= kFwdPick && mode <= kFwdPickCodeDv; }
+__host__ __device__ constexpr bool code_mode(int mode) { return mode == kFwdPickCode || mode == kFwdPickCodeDv; }
 // B operand stored with the output column as the contiguous axis (MN-major)?
 __host__ __device__ constexpr bool b_mn_major(int mode) {
     return mode == kBwdDh || mode == kBwdDw || mode == kBwdDwHalf || mode == kFwdBf16Dv || mode == kBwdPDv || mode == kFwdKeepDv ||
-           mode == kFwdPickDv || mode == kFwdPickKeepDv || mode == kBwdPPickDv;
+           mode == kFwdPickDv || mode == kFwdPickKeepDv || mode == kBwdPPickDv || mode == kFwdPickCodeDv;
 }
 
 constexpr int kSms = 148;                // SMs of the part; the work splits below are planned for it
@@ -95,6 +99,13 @@ constexpr int kPartTileFloats = kDhRows * kBN;
 // (expm1), so a nearly certain token loses nothing to cancellation.
 __host__ __device__ inline bool exp_form(float lse) { return lse >= -20.0f && lse <= 59.0f; }
 __device__ __forceinline__ float exp_form_target(float lp, float lse) { return expm1f(lp) * expf(lse); }
+
+// 16-bit codes of scaled logits: steps of 1/640 from -42 on, 0 for what lies below.  A distillation step that forms dW needs its scratch
+// in the final scale, coef e^(x - lse), and lse is known only when the logits are gone.  A code is off by 1/1280 at most, so its
+// exponential by 8e-4 (4.5e-4 rms, beside the 1.7e-3 of the bf16 that it becomes), and turning codes into scratch is one sweep of 4 bytes per
+// entry where computing the logits again is 2 d multiply-adds: 0.25 against 2.2 ms for 2,305 rows, d = 4096, V = 151936.  Rows
+// outside exp_form's range of lse, whose logits leave that of the codes, are computed again.
+constexpr float kCodeSteps = 640.f, kCodeZero = 42.f;
 
 // Pacing of the CTAs of a launch (lmhead_common.cuh): stage fills per announcement, counters in the ring.
 constexpr int kPaceFills = 16;

@@ -332,8 +332,16 @@ __device__ __forceinline__ void row_slice(const LmheadArgs& a, RowState& r, int 
         }
         r.s = fmaf(r.s, ex2(r.m2 - m_new), add);
         r.m2 = m_new;
-        if (!KEEP || !store || col0 >= a.ncols) return;
-        if (m_new != 0.f) {                            // rare: this range of the row lies far below the rest, or above
+        if (!(KEEP || code_mode(MODE)) || !store || col0 >= a.ncols) return;
+        if (code_mode(MODE)) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+                const uint32_t lo = __float_as_uint(fminf(fmaxf(fmaf(x[i], kCodeSteps, kCodeZero * kCodeSteps), 0.f), 65535.f) + 8388608.f);
+                const uint32_t hi = __float_as_uint(fminf(fmaxf(fmaf(x[i + 1], kCodeSteps, kCodeZero * kCodeSteps), 0.f), 65535.f) + 8388608.f);
+                pk[i >> 1] = (lo & 0xffffu) | (hi << 16);
+            }
+        }
+        if (KEEP && m_new != 0.f) {                    // rare: this range of the row lies far below the rest, or above
 #pragma unroll
             for (int i = 0; i < 32; i += 2)
                 pk[i >> 1] = pack_bf16(ex2(fmaf(x[i], kLog2e, -0.f)), ex2(fmaf(x[i + 1], kLog2e, -0.f)));

@@ -378,6 +378,8 @@ cudaError_t launch_lmhead_pair(int mode, const CUtensorMap& tmA, const CUtensorM
         case kFwdPickKeepDv: return launch<kFwdPickKeepDv>(tmA, tmB, tmB2, args, num_ctas, stream);
         case kBwdPPick: return launch<kBwdPPick>(tmA, tmB, tmB2, args, num_ctas, stream);
         case kBwdPPickDv: return launch<kBwdPPickDv>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPickCode: return launch<kFwdPickCode>(tmA, tmB, tmB2, args, num_ctas, stream);
+        case kFwdPickCodeDv: return launch<kFwdPickCodeDv>(tmA, tmB, tmB2, args, num_ctas, stream);
         case kBwdDwHalf: return launch<kBwdDwHalf>(tmA, tmB, tmB2, args, num_ctas, stream);
     }
     return cudaErrorInvalidValue;
@@ -387,7 +389,7 @@ cudaError_t lmhead_pair_prepare() {
     const cudaError_t all[] = {prepare<kFwdBf16>(), prepare<kFwdBf16Dv>(), prepare<kFwdKeep>(), prepare<kFwdKeepDv>(),
                                prepare<kBwdP>(),    prepare<kBwdPDv>(),    prepare<kFwdFp8T>(),   prepare<kBwdDw>(),
                                prepare<kFwdPick>(), prepare<kFwdPickDv>(), prepare<kFwdPickKeep>(), prepare<kFwdPickKeepDv>(),
-                               prepare<kBwdPPick>(), prepare<kBwdPPickDv>(), prepare<kBwdDwHalf>()};
+                               prepare<kBwdPPick>(), prepare<kBwdPPickDv>(), prepare<kBwdDwHalf>(), prepare<kFwdPickCode>(), prepare<kFwdPickCodeDv>()};
     for (const cudaError_t e : all)
         if (e != cudaSuccess) return e;
     return cudaSuccess;

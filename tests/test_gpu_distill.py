@@ -5,7 +5,8 @@ at most (d / 16) 2^-23 A / tau, A = max_v sum_i |h_i W_vi| of the row (`dx`; the
 more than its logits, plus its fp32 exponentials and sums: 1.5e-5 as in the sampling tests, e^x in the scratch by 2^-22 + 100 x 2^-24
 relative.  So kl: mass (2 dx + 1.5e-5), and 2^-24 of itself for the output.  A scratch entry g is rounded to bf16 once (2^-8 of itself at
 most) after an error of p (2 dx + 2e-5) times the row's factor f = |w| mass / tau; the contraction over n terms cuts its partial
-sums, (n / 16) 2^-23 of sum |g W|; and dH is rounded once more.  dW likewise over the rows.
+sums, (n / 16) 2^-23 of sum |g W|; and dH is rounded once more.  dW likewise over the rows.  With dW the scratch comes from logits in
+steps of 1/640, off by 1/1280: another 8e-4 p f (e^(1/1280) - 1 = 7.8e-4).
 """
 
 import numpy as np
@@ -96,7 +97,8 @@ class Case:
             x = _np(torch.nan_to_num(self.H)) @ _np(self.W).T / self.tau
             p = np.exp(x - x.max(axis=1, keepdims=True))
             p /= p.sum(axis=1, keepdims=True)
-            dg = STEP16 * np.abs(r["g"]) + p * ((2 * dx + 2e-5) * lw * mass / self.tau)[:, None]
+            code = 8e-4 if st.dW is not None else 0.0
+            dg = STEP16 * np.abs(r["g"]) + p * ((2 * dx + 2e-5 + code) * lw * mass / self.tau)[:, None]
         if st.dH is not None:
             tol = dg @ W + (V / 16 + 1) * 2.0 ** -23 * (np.abs(r["g"]) @ W) + 2.0 ** -23 * (p @ W) * (lw * mass / self.tau)[:, None]
             tol += STEP16 * (np.abs(r["dH"]) + tol) + 1e-38
