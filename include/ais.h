@@ -450,7 +450,8 @@ void ais_default_sampling(ais_sampling* how);   /* host pointer; fills in the nu
  * 1e-12 of their size, whatever the type.  mask [rows] (may be NULL): rows with mask 0 give token -1 and zeros.  So do rows without
  * a finite entry (AIS_FLAG_EMPTY), with a NaN or +inf (AIS_FLAG_NONFINITE) or with a parameter of their own out of range
  * (AIS_FLAG_PARAM); the numbers in `how` are checked on the host.
- * No workspace; results do not depend on the other rows of the call.
+ * No workspace.  A row's token and n_kept do not depend on the other rows of the call, its log-probs to the last bits only (the
+ * number of rows decides how many CTAs share one, and so the order of its sums).
  */
 int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t ld, const ais_sampling* how, const float* u,
                const uint8_t* mask, int32_t* tokens, float* lp, float* lp_full, int32_t* n_kept, uint32_t* dev_status, void* stream);

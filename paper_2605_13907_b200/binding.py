@@ -620,6 +620,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
         if torch.is_tensor(value):
             _check_rows(name, value, rows, torch.int32 if name == "top_k" else torch.float32, dev)
             setattr(how, name + "_rows", value.data_ptr())
+        elif name == "top_k":
+            how.top_k = max(0, min(int(value), V))       # (0 or less, and V or more: all)
         else:
             setattr(how, name, value)
     if out is None:
@@ -641,6 +643,8 @@ def top_logits(logits: torch.Tensor, K: int, temperature: float = 1.0, mask: tor
     (include/ais.h, ais_top_logits): what `DistillStep.step` takes as a teacher."""
     rows, V, ld = _check_logits(logits)
     dev = logits.device
+    if not 0 < K <= min(V, TOP_MAX):
+        raise AisError(f"K must lie between 1 and min(V, {TOP_MAX})")
     if mask is not None:
         _check_rows("mask", mask, rows, torch.uint8, dev)
     _check_status(status, dev)

@@ -10,15 +10,16 @@
 // A row belongs to a cluster of one to eight CTAs, a slice each.  What bounds the kernels is one read of the logits for many rows,
 // and the chain of block and cluster barriers for few; so every case reads the row as few times as it can.
 //  * The K largest (top_logits, top-k up to 1,024): one pass.  The first tile of a slice gives a threshold (the K-th largest of the
-//    maxima of 256 to 1,024 groups of entries: K entries reach it), later entries above it join a list in shared memory, and the list is cut
-//    back to its K largest when it fills up, which raises the threshold.  Lists of all slices are sorted together at the end.
+//    maxima of 256 to 1,024 groups of entries: K entries reach it); later 16-byte chunks with an entry above it join a list in shared
+//    memory, and each time the list has doubled the threshold rises to the K-th of the list.  The entries of the listed chunks that
+//    reach the last threshold are sorted, for all slices together, at the end.
 //  * No filter: one pass of fp64 sums per warp, then the one warp's range that holds the token is read again.
 //  * Everything else (top-p or min-p over the whole row, longer top-k, lists that overflow, values out of fp32's range): passes over
-//    data that is mostly still in L1 or L2.  Maximum; histogram of the distance below it (2,048 bins of 1/64 of a unit of log-probability;
-//    a bin is a range of the order); for top-p the counts give bounds on the mass above every bin, and one pass of fp64
-//    exponentials adds up the mass above the bounds per warp and that of the bins between them per bin.  The entries of the bin
-//    with the cut go to one CTA, which sorts them; a bin of more entries than its list holds is first divided by the number
-//    itself, 2,048 ways at a time.
+//    data that is mostly still in L1 or L2.  Maximum; histogram of the distance below it (8,192 bins of 1/256 of a unit of log-
+//    probability; a bin is a range of the order).  For top-p the counts bound the mass above every bin, so the cut lies between two
+//    bins; one pass of fp64 exponentials gives the total and the mass before the first of them; with these the counts put the cut into
+//    one or two bins, whose entries, and those from the first bound on, are listed.  The group around the cut is divided by the
+//    entries' numbers, 1,024 ways at a time, until the few entries left are added up one by one.
 //
 // Precision: which token is drawn and how many are kept are decided by comparing sums over the vocabulary with borders; fp32
 // sums (1e-7 relative) would decide one row in a hundred differently.  Exponentials and sums that decide are fp64, summed in an
@@ -884,8 +885,10 @@ struct Row {
 
     // The K largest entries by one pass: rank 0 gets them sorted in s.list and returns their number, and the fp32 sum of exponentials
     // about `ref` in `full` (all threads of all CTAs).  -1: a list overflowed, or the sum says that the row needs a closer look.
-    // What the pass lists is chunks, by their largest entry (a fifth of the instructions that the entries themselves would take: 592 x 151936
-    // bf16, K = 64, STREAM_US); the K-th of the K chunks listed first bounds the K-th entry from below as well.
+    // What the pass lists is chunks, by their largest entry (a tenth of the instructions that listing entries takes; 613 x 151936
+    // bf16, K = 64: 94 -> 78 us); the K-th largest of them bounds the K-th entry from below as well.
+    // 2,048 x 126464 fp32, K = 8: 205-229 us, 5.0 TB/s; K = 128: 272; 512 x 262144 fp16, K = 50: 89 us, 3.0 TB/s (the exponentials and maxima of
+    // 16-bit entries: 20 instructions per entry and lane before, about 12 now).
     __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
         SelShared& s = smem();
         constexpr int kTile = kSelThreads * kDeep;
@@ -1112,6 +1115,12 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
     if (temperature == 0.f) {
         temperature = 1.f;
         k = 1;
+    }
+    // a top-k of everything is none, unless it makes the whole of a short row the list that the other filters work on
+    if (a.V > kMaxTopLogits) {
+        if (k >= a.V) k = 0;
+    } else if (k <= 0 && (p < 1.f || m > 0.f)) {
+        k = a.V;
     }
     if (a.rows_of != kAllRows && one_pass(k, p, m) != first_kind) return;
     {
@@ -1498,13 +1507,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
 }
 
 template <typename K>
-cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream, int forced = 0) {
+cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream, int forced /* CTAs per row at least, if the row is long enough */ = 0) {
     // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  (Not beyond: the cluster's barriers and the
     // merging cost more than a better filled last wave gives; 613 rows of 151936 bf16, K = 64: one CTA 109 us, four 349.)
     int c = 1;
     while (c < kMaxCluster && rows * c * 2 <= 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
     if (forced > 0)
-        for (c = 1; c < forced && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384; c *= 2) {}
+        for (; c < forced && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384; c *= 2) {}
     a.cluster = c;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(rows * c));
@@ -1589,7 +1598,8 @@ int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t l
                                   : launch_select(sample_kernel<float>, a, rows, 4, s, forced);
     };
     // Rows with filters of their own: the few that need several passes get four CTAs each, in a launch of their own that the others overlap
-    // (256 x 151936 bf16 with mixed parameters: one launch 207 us, two MIXED_US).
+    // (256 x 151936 bf16 with mixed parameters and banned
+    // entries: 146 us; one launch with a CTA per row took as long as its slowest row, 200).
     cudaError_t e = cudaSuccess;
     if (how->top_k_rows || how->top_p_rows || how->min_p_rows) {
         a.rows_of = kManyPasses;

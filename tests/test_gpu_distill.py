@@ -313,6 +313,36 @@ def test_streams_and_captured_graphs():
     assert all(torch.equal(a, b) for a, b in zip(want, (st.kl, st.loss, st.dH, st.dW)))
 
 
+def test_writes_stay_inside_the_buffers():
+    """Outputs and a workspace of the least size, each inside a larger buffer of known bytes; rows of dH and dW with padding between."""
+    ais = _ais()
+    for dv in (False, True):
+        c = Case(150, 256, 1000, 9, seed=21, dv=dv, masked=0.2, ldh=272)
+        want = c.run(c.step(dw=True))
+
+        def inside(shape, dtype, pad=0):
+            n = int(np.prod(shape[:-1])) * (shape[-1] + pad)
+            es = torch.empty(0, dtype=dtype).element_size()
+            raw = torch.full((512 + n * es + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+            return raw, raw[512:512 + n * es].view(dtype).view(*shape[:-1], shape[-1] + pad)[..., :shape[-1]]
+
+        T, d, V = 150, 256, 1000
+        raws, out = zip(*(inside((T,), torch.float32), inside((T,), torch.float32), inside((1,), torch.float32), inside((T, d), torch.bfloat16, 16),
+                          inside((d, V) if dv else (V, d), torch.bfloat16, 24)))
+        size = ais.distill_workspace_min_bytes(want.shape, 9, ais.DISTILL_DH | ais.DISTILL_DW)
+        ws_raw, ws = inside((size,), torch.uint8)
+        kl, lse, loss, dH, dW = out
+        ais.distill(want.shape, c.H, c.head(), c.ids, c.logits, c.mask, kl, loss, ws, lse=lse, dH=dH, dW=dW)
+        torch.cuda.synchronize()
+        for got, ref in zip(out, (want.kl, want.lse, want.loss, want.dH, want.dW)):
+            assert torch.equal(got, ref)
+        for raw in raws + (ws_raw,):
+            assert (raw[:512] == 0x5A).all() and (raw[-512:] == 0x5A).all()
+        for raw, rows, cols, pad in ((raws[3], T, d, 16), (raws[4], d if dv else V, V if dv else d, 24)):
+            body = raw[512:-512].view(rows, (cols + pad) * 2)[:, cols * 2:]
+            assert (body == 0x5A).all()
+
+
 def test_refusals_of_the_python_layer():
     ais = _ais()
     c = Case(10, 128, 512, 4, seed=19)

@@ -218,6 +218,68 @@ def test_streams_and_captured_graphs():
         assert all(torch.equal(p, q) for p, q in zip(out, ais.sample(a, b, top_k=50, top_p=0.9)))
 
 
+def test_captured_with_parameters_of_their_own_behind_a_kernel_that_writes_them():
+    """Two launches that overlap: both see what the kernels before them wrote, and the kernel behind them sees both."""
+    ais = _ais()
+    rows, V = 300, 20011
+    x, u = _logits(rows, V, "bf16", 30), _u(rows, 31)
+    rng = np.random.default_rng(32)
+    k = torch.from_numpy(rng.choice([0, 5, 2000], rows).astype(np.int32)).cuda()
+    p = torch.from_numpy(rng.choice([0.5, 0.9, 1.0], rows).astype(np.float32)).cuda()
+    src = torch.empty_like(x)
+    out = ais.Sampled(*(torch.zeros(rows, dtype=t, device="cuda") for t in (torch.int32, torch.float32, torch.float32, torch.int32)))
+    seen = torch.zeros(rows, dtype=torch.int32, device="cuda")
+
+    def go():
+        src.copy_(x)
+        ais.sample(src, u, top_k=k, top_p=p, out=out)
+        seen.copy_(out.tokens)
+        src.zero_()
+
+    go()
+    torch.cuda.synchronize()
+    want = seen.clone()
+    _check(x, u, out, torch.zeros(1, dtype=torch.int32), top_k=k.tolist(), top_p=p.tolist())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            go()
+    for _ in range(5):
+        seen.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(seen, want)
+
+
+def test_two_streams_at_once():
+    ais = _ais()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    x, u = _logits(64, 50003, "fp32", 33), _u(64, 34)
+    want = ais.sample(x, u, top_p=0.9), ais.top_logits(x, 50)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        with torch.cuda.stream(a):
+            got.append((ais.sample(x, u, top_p=0.9), want[0]))
+        with torch.cuda.stream(b):
+            got.append((ais.top_logits(x, 50), want[1]))
+    torch.cuda.synchronize()
+    for g, w in got:
+        assert all(torch.equal(p, q) for p, q in zip(g, w))
+
+
+def test_an_ascending_row_and_a_descending_one():
+    """Every entry beats those before it: the list of the largest overflows; and the other way round."""
+    ais = _ais()
+    V = 131072
+    x = torch.stack([torch.arange(V), torch.arange(V).flip(0)]).float().cuda() * 1e-4
+    for K in (1, 64, 1024):
+        _check_top(x, K, 1.0, ais.top_logits(x, K))
+    u = _u(2, 35)
+    for how in (dict(top_k=100, top_p=0.9), dict(top_p=0.5), dict(top_k=3000), dict(min_p=0.2)):
+        _check(x, u, *_sample(x, u, **how), **how)
+
+
 # ------------------------------------------------------------------------------------------ top logits
 def _check_top(x, K, tau, r):
     for i, row in enumerate(_np(x)):
