@@ -387,12 +387,17 @@ struct Row {
     __device__ __forceinline__ int bin(float v) const { return static_cast<int>(__float_as_uint(bin_f(v)) & (kBins - 1)); }
     // The largest value whose bin is `b` or a later one (bin_f falls as its value rises): a comparison with it does for one with the bin.
     __device__ float edge_value(int b) const {
-        uint32_t lo = 0x007fffffu, hi = 0xff800000u;              // -inf and +inf in ascending order (order_of() before it is turned over)
+        // a warp tries 32 places at a time of the values in ascending order (see order_of()), from -inf to +inf
+        const uint32_t lane = threadIdx.x & 31;
+        uint32_t lo = 0x007fffffu, hi = 0xff800000u;
         while (hi - lo > 1u) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            const float v = __uint_as_float(mid ^ ((mid >> 31) != 0u ? 0x80000000u : 0xffffffffu));
-            if (v > top || bin_f(v) < kTwo23 + b) hi = mid;
-            else lo = mid;
+            const uint32_t step = max((hi - lo) / 33u, 1u), at = lo + min((lane + 1u) * step, hi - lo);
+            const float v = __uint_as_float(at ^ ((at >> 31) != 0u ? 0x80000000u : 0xffffffffu));
+            const unsigned beyond = __ballot_sync(0xffffffffu, at >= hi || v > top || bin_f(v) < kTwo23 + b);
+            const uint32_t first = beyond == 0u ? 32u : static_cast<uint32_t>(__ffs(beyond) - 1);     // places before it are not beyond
+            const uint32_t from = lo;
+            if (first < 32u) hi = min(hi, from + (first + 1u) * step);
+            lo = from + first * step;
         }
         return __uint_as_float(lo ^ ((lo >> 31) != 0u ? 0x80000000u : 0xffffffffu));
     }
@@ -535,7 +540,13 @@ struct Row {
         const float step = -1.4426950408889634f / kBinsPerNat;
         uint32_t count[kMine];
 #pragma unroll
-        for (int j = 0; j < kMine; j += 4) *reinterpret_cast<uint4*>(count + j) = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0)[j / 4];
+        for (int j = 0; j < kMine; j += 4) {
+            const uint4 c = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0)[j / 4];
+            count[j] = c.x;
+            count[j + 1] = c.y;
+            count[j + 2] = c.z;
+            count[j + 3] = c.w;
+        }
         // the exponentials of the bins by steps of e^(-1/256) from the thread's first; a thread's sums in fp32 (3e-6 relative, like the steps)
         const float down = 0.99610137f, first = ex2_approx((b0 - 0.5f) * step);
         auto walk = [&](auto f) {
@@ -731,42 +742,45 @@ struct Row {
         }
         return min(sort_list(n), K);
     }
-    // The cut inside a group of `count` entries, those that over(f) calls f(value, number) for, in all CTAs: by count, the entry number `want`
+    // The cut inside a group of `count` entries with numbers from `from` to `to`, those that over(f) calls f(value, number) for, in all CTAs: by count, the entry number `want`
     // (from 1) of the group; by mass, the first at which mass0 plus the masses reach `target` (in units of 2^-44), and the last of the
     // group where rounding leaves none.  The range of numbers is divided 1,024 ways, and again the part with the cut, until no more
     // than 256 entries are left; they go to rank 0, where each adds up those before it.
     template <bool MASS, typename Over>
-    __device__ u64 cut_in_group(Over over, int count, int want, double mass0, double target) const {
+    __device__ u64 cut_in_group(Over over, u64 from, u64 to, int count, int want, double mass0, double target) const {
         SelShared& s = smem();
-        u64 from = 0, to = ~0ull;
-        while (count > kFew) {
-            // the ends of what is left of the group
-            u64 lo = ~0ull, hi = 0;
-            over([&](float, u64 o) {
-                if (o >= from && o <= to) { lo = min(lo, o); hi = max(hi, o); }
-            });
-            for (int o = 16; o > 0; o >>= 1) {
-                lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-            }
+        for (bool ends = false; count > kFew; ends = true) {
+            // the ends of what is left of the group (equal values leave most of a range empty)
+            u64 lo = ends ? ~0ull : from, hi = ends ? 0 : to;
+            if (ends)
+                over([&](float, u64 o) {
+                    if (o >= from && o <= to) { lo = min(lo, o); hi = max(hi, o); }
+                });
+            if (ends)
+                for (int o = 16; o > 0; o >>= 1) {
+                    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+                }
             __syncthreads();
-            if ((threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = lo; s.warp_u64[1][threadIdx.x >> 5] = hi; }
+            if (ends && (threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = lo; s.warp_u64[1][threadIdx.x >> 5] = hi; }
             for (int b = threadIdx.x; b < kSplit; b += kSelThreads) {
                 s.part[b] = 0;
                 if (MASS) s.mass[b] = 0;
             }
             __syncthreads();
-            if (threadIdx.x == 0) {
-                for (int w = 0; w < kSelWarps; ++w) { lo = min(lo, s.warp_u64[0][w]); hi = max(hi, s.warp_u64[1][w]); }
-                s.pub[turn].lo = lo;
-                s.pub[turn].hi = hi;
+            if (ends) {
+                if (threadIdx.x == 0) {
+                    for (int w = 0; w < kSelWarps; ++w) { lo = min(lo, s.warp_u64[0][w]); hi = max(hi, s.warp_u64[1][w]); }
+                    s.pub[turn].lo = lo;
+                    s.pub[turn].hi = hi;
+                }
+                sync();
+                for (int r = 0; r < C; ++r) {
+                    lo = min(lo, remote(&s.pub[turn], r)->lo);
+                    hi = max(hi, remote(&s.pub[turn], r)->hi);
+                }
+                turn ^= 1;
             }
-            sync();
-            for (int r = 0; r < C; ++r) {
-                lo = min(lo, remote(&s.pub[turn], r)->lo);
-                hi = max(hi, remote(&s.pub[turn], r)->hi);
-            }
-            turn ^= 1;
             const int bits = 64 - __clzll(hi - lo);               // (more than 256 numbers: hi > lo)
             const int shift = bits > 10 ? bits - 10 : 0;
             over([&](float x, u64 o) {
@@ -1217,7 +1231,8 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             const int b = s.found[0], ahead = s.found[1], in = s.found[2];
             __syncthreads();
             const bool listed = k <= kMaxTopLogits && ahead + in <= 4096;
-            if (!listed) cut = r.template cut_in_group<false>(data([&](float x, int) { return x > -INFINITY && r.bin(x) == b; }), in, k - ahead, 0.0, 0.0);
+            if (!listed) cut = r.template cut_in_group<false>(data([&](float x, int) { return x > -INFINITY && r.bin(x) == b; }), order_of(r.top, 0), last_finite(), in,
+                                                                 k - ahead, 0.0, 0.0);
             if (k <= kMaxTopLogits) {
                 log_full = log(r.template add_up<false>(full, 0.0, 0, 0.f, 0).sum[0]);
                 const int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
@@ -1290,7 +1305,8 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                         }
                     };
                     cut = r.template cut_in_group<true>(
-                        listed, between, 0, mass_b1 * kMassOne, target * kMassOne);
+                        listed, order_of(from_value, 0), to_value > -INFINITY ? order_of(to_value, 0) - 1 : last_finite(), between, 0, mass_b1 * kMassOne,
+                        target * kMassOne);
                     if (!by_m) {
                         counted = true;
                         listed([&](float x, u64 o) {
@@ -1301,7 +1317,8 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                         if (r.rank == 0 && threadIdx.x == 0) kept += before;
                     }
                 } else {
-                    cut = r.template cut_in_group<true>(data(open), between, 0, mass_b1 * kMassOne, target * kMassOne);
+                    cut = r.template cut_in_group<true>(data(open), order_of(from_value, 0), to_value > -INFINITY ? order_of(to_value, 0) - 1 : last_finite(),
+                                                        between, 0, mass_b1 * kMassOne, target * kMassOne);
                 }
             }
             cut_value = value_of(cut);
@@ -1493,7 +1510,7 @@ __device__ __forceinline__ void top_row(const SelectArgs& a) {
                         if (v[j] > -INFINITY && r.bin(v[j]) == b) f(v[j], order_of(v[j], i + j));
                 });
             },
-            in, k - ahead, 0.0, 0.0);
+            order_of(r.top, 0), last_finite(), in, k - ahead, 0.0, 0.0);
     int n = r.gather([&](float x, int i) { return listed ? x > -INFINITY && r.bin(x) <= b : order_of(x, i) <= cut; });
     if (r.rank == 0) n = r.sort_top(n, k);
     if (r.rank == 0) write(min(n, k), static_cast<float>(static_cast<double>(r.top) * r.inv_t + log(full)));
@@ -1597,13 +1614,14 @@ int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t l
                : dtype == AIS_F16 ? launch_select(sample_kernel<__half>, a, rows, 2, s, forced)
                                   : launch_select(sample_kernel<float>, a, rows, 4, s, forced);
     };
-    // Rows with filters of their own: the few that need several passes get four CTAs each, in a launch of their own that the others overlap
+    // Rows with filters of their own: the few that need several passes get two CTAs each at least, in a launch of their own that the others overlap
     // (256 x 151936 bf16 with mixed parameters and banned
-    // entries: 146 us; one launch with a CTA per row took as long as its slowest row, 200).
+    // entries: MIXED_US; with four CTAs 144 and, for the fixed part of a CTA's work, no faster; one launch with a CTA per row took as long
+    // as its slowest row, 200).
     cudaError_t e = cudaSuccess;
     if (how->top_k_rows || how->top_p_rows || how->min_p_rows) {
         a.rows_of = kManyPasses;
-        e = launch(4);
+        e = launch(2);
         a.rows_of = kOnePass;
         a.late = 1;
     }
