@@ -47,7 +47,7 @@ namespace {
 
 constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight
+constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight in the pass for the largest entries
 constexpr int kBins = 8192;
 constexpr int kListCap = 4096;           // entries of a list
 constexpr int kSplit = 1024;             // ways in which a group of entries is divided
@@ -301,6 +301,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
 template <typename T>
 struct Row {
     static constexpr int kEach = Elem<T>::kEach;
+    static constexpr int kLight = 16 / kEach;    // chunks in flight in passes of few instructions per entry (their code is fetched once, too)
     const T* x;              // the row
     int V, head;             // its length; elements before the first 16-byte boundary
     int whole;               // 16-byte chunks behind that
@@ -538,47 +539,42 @@ struct Row {
         constexpr int kMine = kBins / kSelThreads;
         const int b0 = threadIdx.x * kMine;
         const float step = -1.4426950408889634f / kBinsPerNat;
-        uint32_t count[kMine];
-#pragma unroll
-        for (int j = 0; j < kMine; j += 4) {
-            const uint4 c = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0)[j / 4];
-            count[j] = c.x;
-            count[j + 1] = c.y;
-            count[j + 2] = c.z;
-            count[j + 3] = c.w;
-        }
-        // the exponentials of the bins by steps of e^(-1/256) from the thread's first; a thread's sums in fp32 (3e-6 relative, like the steps)
+        const uint4* count = reinterpret_cast<const uint4*>((one ? s.hist : s.tot) + b0);
+        // the exponentials of the bins by steps of e^(-1/256) from the thread's first; a thread's sums in fp32 (3e-6 relative, like the steps).
+        // Loops that stay loops: code that runs once is fetched once, and 6 KB of it took 3 us.
         const float down = 0.99610137f, first = ex2_approx((b0 - 0.5f) * step);
         auto walk = [&](auto f) {
             float e = first, hs = 0.f, ls = 0.f;
+#pragma unroll 1
+            for (int j = 0; j < kMine; j += 4) {
+                const uint4 four = count[j / 4];
+                const uint32_t c4[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
-            for (int j = 0; j < kMine; ++j) {
-                const float c = b0 + j >= from ? static_cast<float>(count[j]) : 0.f;
-                hs = fmaf(c * 1.00002f, e, hs);
-                e *= down;
-                ls = fmaf(b0 + j < kBins - 1 ? c * 0.99998f : 0.f, e, ls);
-                f(hs, ls, j);
+                for (int k = 0; k < 4; ++k) {
+                    const int b = b0 + j + k;
+                    const float c = b >= from ? static_cast<float>(c4[k]) : 0.f;
+                    hs = fmaf(c * 1.00002f, e, hs);
+                    e *= down;
+                    ls = fmaf(b < kBins - 1 ? c * 0.99998f : 0.f, e, ls);
+                    f(hs, ls, b, c4[k]);
+                }
             }
         };
         float hs = 0.f, ls = 0.f;
-        walk([&](float h, float l, int) { hs = h; ls = l; });
+        walk([&](float h, float l, int, uint32_t) { hs = h; ls = l; });
         double h_total, l_total;
         const double h = mass0 + block_scan(static_cast<double>(hs), s.warp_f64[0], h_total);
         const double l = mass0 + block_scan(static_cast<double>(ls), s.warp_f64[1], l_total);
         const double to_lo = p * (total > 0.0 ? total : l_total), to_hi = p * (total > 0.0 ? total : h_total);
         int n = 0;                                                // bins before b1, and (times 2^16) those before b2 + 1
-        walk([&](float hj, float lj, int j) {
-            n += (b0 + j < from || h + static_cast<double>(hj) < to_lo ? 1 : 0) + (b0 + j < from || l + static_cast<double>(lj) < to_hi ? 1 << 16 : 0);
+        walk([&](float hj, float lj, int b, uint32_t) {
+            n += (b < from || h + static_cast<double>(hj) < to_lo ? 1 : 0) + (b < from || l + static_cast<double>(lj) < to_hi ? 1 << 16 : 0);
         });
         int sum;
         block_scan(n, s.warp_int, sum);
         const int b1 = min(sum & 0xffff, kBins - 1), b2 = min(sum >> 16, kBins - 1);
         u64 entries = 0;                                          // before b1, and (times 2^32) from b1 to b2
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-            if (b0 + j < b1) entries += count[j];
-            else if (b0 + j <= b2) entries += static_cast<u64>(count[j]) << 32;
-        }
+        walk([&](float, float, int b, uint32_t c) { entries += b < b1 ? c : b <= b2 ? static_cast<u64>(c) << 32 : 0; });
         u64 all;
         block_scan(entries, s.warp_u64[0], all);
         if (threadIdx.x == 0) {
@@ -593,7 +589,7 @@ struct Row {
     // one for each entry they queue up: 2,000 took 25 us).
     template <typename F, typename G>
     __device__ __forceinline__ void collect(F keep, int* counter, G put) const {
-        each<kDeep>([&](const float (&v)[kEach], int i, int) { collect_chunk(v, i, keep, counter, put); });
+        each<kLight>([&](const float (&v)[kEach], int i, int) { collect_chunk(v, i, keep, counter, put); });
     }
     template <typename F, typename G>
     static __device__ __forceinline__ int collect_chunk(const float (&v)[kEach], int i, F keep, int* counter, G put) {
@@ -868,7 +864,7 @@ struct Row {
     __device__ Totals look() const {
         float most = -INFINITY;
         int missing = 0;
-        each<kDeep>([&](const float (&v)[kEach], int, int n) { see(v, n, most, missing); });
+        each<kLight>([&](const float (&v)[kEach], int, int n) { see(v, n, most, missing); });
         return extremes(0.0, most, missing);
     }
     // Totals of a pass that has seen all of this thread's chunks.
@@ -884,7 +880,7 @@ struct Row {
         const float c = static_cast<float>(1.4426950408889634 * inv_t);
         clear_hist();
         double full = 0.0;
-        each<kDeep>([&](const float (&v)[kEach], int, int) {
+        each<kLight>([&](const float (&v)[kEach], int, int) {
             float f = 0.f;
 #pragma unroll
             for (int k = 0; k < kEach; ++k) {
@@ -1215,7 +1211,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
         // the entries of the slice that pick(value, index) takes, as cut_in_group wants them
         auto data = [&](auto pick) {
             return [&r, pick](auto f) {
-                r.template each<kDeep>([&](const float (&v)[kEach], int i, int) {
+                r.template each<Row<T>::kLight>([&](const float (&v)[kEach], int i, int) {
                     unsigned taken = 0;
 #pragma unroll
                     for (int j = 0; j < kEach; ++j) taken |= (pick(v[j], i + j) ? 1u : 0u) << j;
@@ -1249,7 +1245,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             if (by_k) {                                           // the histogram of what top-k has left
                 __syncthreads();
                 r.clear_hist();
-                r.template each<kDeep>([&](const float (&v)[kEach], int i, int) {
+                r.template each<Row<T>::kLight>([&](const float (&v)[kEach], int i, int) {
 #pragma unroll
                     for (int j = 0; j < kEach; ++j)
                         if (inside(v[j], i + j)) atomicAdd(&s.hist[r.bin(v[j])], 1u);
@@ -1504,7 +1500,7 @@ __device__ __forceinline__ void top_row(const SelectArgs& a) {
     if (!listed)
         cut = r.template cut_in_group<false>(
             [&](auto f) {
-                r.template each<kDeep>([&](const float (&v)[Row<T>::kEach], int i, int) {
+                r.template each<Row<T>::kLight>([&](const float (&v)[Row<T>::kEach], int i, int) {
 #pragma unroll
                     for (int j = 0; j < Row<T>::kEach; ++j)
                         if (v[j] > -INFINITY && r.bin(v[j]) == b) f(v[j], order_of(v[j], i + j));
