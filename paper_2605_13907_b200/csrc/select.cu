@@ -301,7 +301,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
 template <typename T>
 struct Row {
     static constexpr int kEach = Elem<T>::kEach;
-    static constexpr int kLight = 16 / kEach;    // chunks in flight in passes of few instructions per entry (their code is fetched once, too)
+    static constexpr int kLight = 16 / kEach;    // chunks in flight in passes of few instructions per entry,
+    static constexpr int kHeavy = 8 / kEach;     // and in those with fp64 exponentials (see each())
     const T* x;              // the row
     int V, head;             // its length; elements before the first 16-byte boundary
     int whole;               // 16-byte chunks behind that
@@ -349,8 +350,9 @@ struct Row {
         to = min(from + per, c1);
     }
     // f(values, index of the first, how many are part of the row) for everything this warp owns, a thread at a time, B chunks of it in flight.
-    // A chunk's registers are loaded again as soon as it is unpacked: handing them on by moves would wait for the load.  B is 4 where
-    // f is short; with the exponentials 2 (four times eight of them did not fit the instruction cache).
+    // A chunk's registers are loaded again as soon as it is unpacked: handing them on by moves would wait for the load.  The code of f is
+    // there B + 1 times, and fetching it counts, most code here running once per row: four chunks of eight 16-bit entries instead of
+    // two took a twelfth longer (256 x 151936 bf16, top-p), four times eight fp64 exponentials twice as long.
     template <int B, typename F>
     __device__ __forceinline__ void each(F f) const {
         int from, to;
@@ -1177,7 +1179,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             double sum = 0.0;
             float most = -INFINITY;
             int missing = 0;
-            r.template each<2>([&](const float (&v)[kEach], int, int n) {
+            r.template each<Row<T>::kHeavy>([&](const float (&v)[kEach], int, int n) {
                 r.see(v, n, most, missing);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
@@ -1260,7 +1262,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             const float from_value = r.edge_value(b1);            // values above it lie in the bins before b1
             double all = 0.0;
             auto add = [&](auto limited) {
-                r.template each<2>([&](const float (&v)[kEach], int i, int) {
+                r.template each<Row<T>::kHeavy>([&](const float (&v)[kEach], int i, int) {
 #pragma unroll
                     for (int j = 0; j < kEach; ++j) {
                         bool in = v[j] >= r.weight.floor;
@@ -1326,7 +1328,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             const float m_floor = by_m ? static_cast<float>(m_from - 1e-6 * (fabs(static_cast<double>(r.top)) + fabs(m_from)) - 1e-30) : -INFINITY;
             const float c = static_cast<float>(1.4426950408889634 * r.inv_t);
             const bool sum_full = !by_k && !by_p;
-            r.template each<2>([&](const float (&v)[kEach], int i, int) {
+            r.template each<Row<T>::kHeavy>([&](const float (&v)[kEach], int i, int) {
                 float f = 0.f;
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
@@ -1610,10 +1612,9 @@ int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t l
                : dtype == AIS_F16 ? launch_select(sample_kernel<__half>, a, rows, 2, s, forced)
                                   : launch_select(sample_kernel<float>, a, rows, 4, s, forced);
     };
-    // Rows with filters of their own: the few that need several passes get two CTAs each at least, in a launch of their own that the others overlap
-    // (256 x 151936 bf16 with mixed parameters and banned
-    // entries: MIXED_US; with four CTAs 144 and, for the fixed part of a CTA's work, no faster; one launch with a CTA per row took as long
-    // as its slowest row, 200).
+    // Rows with filters of their own: the few that need several passes get two CTAs each at least, in a launch of their own that the
+    // others overlap (256 x 151936 bf16 with mixed parameters and banned entries: 127 us, with four CTAs 133; in one launch with a CTA
+    // per row it took as long as its slowest row, 200).
     cudaError_t e = cudaSuccess;
     if (how->top_k_rows || how->top_p_rows || how->min_p_rows) {
         a.rows_of = kManyPasses;
