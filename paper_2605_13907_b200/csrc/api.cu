@@ -1158,15 +1158,15 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
         return AIS_OK;
     }
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    uint32_t* counters = reinterpret_cast<uint32_t*>(ws + L.off_counters);       // rows of the batch, rows to recompute, ticket
+    uint32_t* counters = reinterpret_cast<uint32_t*>(ws + L.off_counters);       // rows to recompute, ticket
     int32_t* sorted_ids = reinterpret_cast<int32_t*>(ws + L.off_ids);
     float* pick = reinterpret_cast<float*>(ws + L.off_pick);
     __nv_bfloat16* U = reinterpret_cast<__nv_bfloat16*>(ws + L.off_u);
     const bool keep = dH && !dW;                                 // the forward pass leaves the exponentials for the dH pass
     const int64_t blk_rows = grads == 0 ? T : scratch_rows(L, T, workspace_bytes);
 
-    const FlagsJob flags = {mask, T, ws + L.off_flags, ws + L.off_pace, static_cast<int64_t>(L.clear_bytes), AdvJob{}};
-    const TeacherJob teacher = {ids, logits, dtype, ldk, K, shape->V, T, mask, sorted_ids, reinterpret_cast<float*>(ws + L.off_logits), counters, dev_status};
+    const TeacherJob teacher = {ids, logits, dtype, ldk, K, shape->V, T, mask, sorted_ids, reinterpret_cast<float*>(ws + L.off_logits),
+                                ws + L.off_flags, ws + L.off_pace, static_cast<int64_t>(L.clear_bytes), dev_status};
     CUtensorMap tmW_k, tmW_n, tmW_tail, tmU;                     // as in loss_bwd
     if (!(dv ? make_tmap_blocks(&tmW_k, W, whole_blocks(V), d, shape->ldw * 2) &&
                    make_tmap(&tmW_tail, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, W, V, d, shape->ldw * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B)
@@ -1176,7 +1176,7 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
                     : make_tmap_blocks(&tmW_n, W, d, V, shape->ldw * 2)) ||
                !make_tmap(&tmU, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, U, V, static_cast<uint64_t>(blk_rows), L.ldU * 2, 64, kBM, CU_TENSOR_MAP_SWIZZLE_128B)))
         return AIS_ERR_DEVICE;
-    if (launch_flags(flags, s) != cudaSuccess || launch_teacher(teacher, s) != cudaSuccess) return AIS_ERR_DEVICE;
+    if (launch_teacher(teacher, s) != cudaSuccess) return AIS_ERR_DEVICE;
 
     DistillJob job = {};
     job.K = K;
@@ -1188,7 +1188,8 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
     job.pick = pick;
     job.teacher_lse = teacher_lse;
     job.weights = weights;
-    job.n_valid = counters;
+    job.tile_rows = ws + L.off_flags;
+    job.tiles = static_cast<int32_t>((T + kBM - 1) / kBM);
     job.kl = kl;
     job.lse = lse;
     job.row_lse = reinterpret_cast<float*>(ws + L.off_lse);
@@ -1198,10 +1199,10 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
     job.ldU = L.ldU;
     job.redo = grads != 0;
     job.redo_flags = ws + L.off_redo;
-    job.redo_count = counters + 1;
+    job.redo_count = counters;
     job.partials = reinterpret_cast<double*>(ws + L.off_partials);
     job.n_partials = static_cast<int32_t>((T + kDistillRows - 1) / kDistillRows);
-    job.ticket = counters + 2;
+    job.ticket = counters + 1;
     job.loss = loss;
     job.status = dev_status;
 

@@ -32,11 +32,18 @@ __device__ __forceinline__ float load_logit(const void* p, int dtype, int64_t i)
 // A warp sorts the (id, position) pairs of a row; n2 is K rounded up to a power of two.
 __global__ void __launch_bounds__(kTeacherWarps * 32) teacher_kernel(const TeacherJob a, int n2) {
     extern __shared__ unsigned long long keys_all[];
-    __shared__ unsigned rows_valid;
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) rows_valid = 0;
-    __syncthreads();
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < a.clear_bytes / 16; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+        static_cast<uint4*>(a.clear)[i] = make_uint4(0, 0, 0, 0);
+    if (warp == 0 && static_cast<int64_t>(blockIdx.x) * kBM < a.T) {
+        int rows = 0;
+        for (int j = 0; j < kBM; j += 32) {
+            const int64_t t = static_cast<int64_t>(blockIdx.x) * kBM + j + lane;
+            rows += __popc(__ballot_sync(0xffffffffu, t < a.T && a.mask[t] != 0));
+        }
+        if (lane == 0) a.tile_rows[blockIdx.x] = static_cast<uint8_t>(rows);      // (128 at most)
+    }
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kTeacherWarps + warp;
     if (t < a.T && a.mask[t] != 0) {
         unsigned long long* keys = keys_all + warp * n2;
@@ -67,10 +74,7 @@ __global__ void __launch_bounds__(kTeacherWarps * 32) teacher_kernel(const Teach
             a.sorted_logits[t * a.K + k] = id >= 0 && id < a.V ? load_logit(a.logits, a.dtype, t * a.ldk + static_cast<uint32_t>(key)) : -INFINITY;
         }
         if (__any_sync(0xffffffffu, beyond) && lane == 0 && a.status) atomicOr(a.status, AIS_FLAG_TOKEN_RANGE);
-        if (lane == 0) atomicAdd(&rows_valid, 1u);
     }
-    __syncthreads();
-    if (threadIdx.x == 0 && rows_valid != 0) atomicAdd(a.n_valid, rows_valid);
 }
 
 __device__ __forceinline__ double warp_add(double v) {
@@ -84,9 +88,17 @@ __device__ __forceinline__ float warp_max(float v) {
 
 __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const __grid_constant__ DistillJob a) {
     __shared__ double row_loss[kDistillRows];
+    __shared__ int warp_rows[kDistillRows];
     __shared__ bool last;
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int n_valid = 0;                                              // rows of the batch with mask 1
+    for (int i = threadIdx.x; i < a.tiles; i += kDistillRows * 32) n_valid += a.tile_rows[i];
+    n_valid = __reduce_add_sync(0xffffffffu, n_valid);
+    if (lane == 0) warp_rows[warp] = n_valid;
+    __syncthreads();
+    n_valid = 0;
+    for (int i = 0; i < kDistillRows; ++i) n_valid += warp_rows[i];
     const int64_t lrow = static_cast<int64_t>(blockIdx.x) * kDistillRows + warp, t = a.row0 + lrow;
     double contribution = 0.0;
     if (lrow < a.rows) {
@@ -130,7 +142,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                     if (r > 0.0) sum += r * (log_r + log_mass - static_cast<double>(a.pick[at + k]) + lse);
                 }
             sum = mass * warp_add(sum);
-            const double w = a.weights ? static_cast<double>(a.weights[t]) : 1.0 / static_cast<double>(*a.n_valid);
+            const double w = a.weights ? static_cast<double>(a.weights[t]) : 1.0 / static_cast<double>(n_valid);
             const bool good = !nan && isfinite(lse) && isfinite(sum) && isfinite(mass) && isfinite(w);
             lse_out = good ? static_cast<float>(lse) : NAN;
             if (!good && lane == 0 && a.status) atomicOr(a.status, AIS_FLAG_NONFINITE);
@@ -190,7 +202,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
         double all = 0.0;
         for (int i = 0; i < kDistillRows; ++i) all += row_loss[i];
         if (a.loss) *a.loss = static_cast<float>(all);
-        if (*a.n_valid == 0 && a.status) atomicOr(a.status, AIS_FLAG_EMPTY);
+        if (n_valid == 0 && a.status) atomicOr(a.status, AIS_FLAG_EMPTY);
     }
 }
 

@@ -7,7 +7,8 @@
 
 namespace ais {
 
-// A teacher's entries of every row brought into the order that the tensor-core epilogues walk: ids ascending, the logits along.
+// Opening of a distillation step: a teacher's entries of every row brought into the order that the tensor-core epilogues walk, ids ascending,
+// the logits along; the rows of every 128-row tile counted; `clear` (16-byte words) zeroed.
 struct TeacherJob {
     const int32_t* ids;
     const void* logits;
@@ -18,7 +19,9 @@ struct TeacherJob {
     const uint8_t* mask;
     int32_t* sorted_ids;       // [T][K]; negative and out-of-range ids keep their place in the order
     float* sorted_logits;      // [T][K]; -inf for entries that do not count
-    uint32_t* n_valid;         // zeroed before: rows with mask 1
+    uint8_t* tile_rows;        // rows with mask 1 of every tile
+    void* clear;
+    int64_t clear_bytes;
     uint32_t* status;
 };
 cudaError_t launch_teacher(const TeacherJob& job, cudaStream_t stream);
@@ -38,7 +41,8 @@ struct DistillJob {
     float* pick;               // [T][K]: scaled student logits in, scratch values out
     const float* teacher_lse;
     const float* weights;
-    const uint32_t* n_valid;
+    const uint8_t* tile_rows;  // [ceil(T / 128)] rows with mask 1
+    int32_t tiles;
     float *kl, *lse;           // lse may be NULL
     float* row_lse;            // [T] workspace: lse of every row, for the recompute pass
     float* coef;               // [T] workspace: w M / tau
@@ -57,7 +61,7 @@ struct DistillJob {
 constexpr int kDistillRows = 8;         // rows of a block (a warp each)
 cudaError_t launch_distill_rows(const DistillJob& job, cudaStream_t stream);
 
-// Scratch rows of codes (logit_code in lmhead.cuh) to coef e^(x - lse), and what pick holds at the listed columns; zeros for rows with coef 0.
+// Scratch rows of codes (kCodeSteps in lmhead.cuh) to coef e^(x - lse), and what pick holds at the listed columns; zeros for rows with coef 0.
 // All per-row arrays begin at the first row of the scratch.
 struct ExpandJob {
     __nv_bfloat16* U;

@@ -33,7 +33,7 @@ enum LmheadMode : int {
     kFwdPickKeepDv = 16,
     kBwdPPick      = 17,
     kBwdPPickDv    = 18,
-    // the forward pass that also leaves 16-bit codes of the scaled logits in the scratch (logit_code)
+    // the forward pass that also leaves 16-bit codes of the scaled logits in the scratch (kCodeSteps)
     kFwdPickCode   = 19,
     kFwdPickCodeDv = 20,
     // the dW pass with a bf16 result
@@ -42,7 +42,9 @@ enum LmheadMode : int {
 
 // What a mode computes (its epilogue and work-unit shape), whatever the layout of W.
 __host__ __device__ constexpr int base_mode(int mode) {
-    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv || (mode >= kFwdPick && mode <= kFwdPickKeepDv) || mode == kFwdPickCode || mode == kFwdPickCodeDv ? kFwdBf16
+    return mode == kFwdBf16Dv || mode == kFwdKeep || mode == kFwdKeepDv || (mode >= kFwdPick && mode <= kFwdPickKeepDv) ||
+                   mode == kFwdPickCode || mode == kFwdPickCodeDv
+               ? kFwdBf16
            : mode == kBwdPDv || mode == kBwdPPick || mode == kBwdPPickDv                                                ? kBwdP
            : mode == kBwdDhDv                                                                                           ? kBwdDh
            : mode == kBwdDwHalf                                                                                         ? kBwdDw

@@ -51,7 +51,7 @@ constexpr int kDeep = 4;                 // 16-byte loads of a thread in flight 
 constexpr int kBins = 8192;
 constexpr int kListCap = 4096;           // entries of a list
 constexpr int kSplit = 1024;             // ways in which a group of entries is divided
-constexpr int kChunkCap = 3072;          // chunks in the list of a pass for the largest entries
+constexpr int kChunkCap = 3200;          // chunks in the list of a pass for the largest entries
 constexpr int kChunkPrune = 2048;        // which is cut back beyond this
 constexpr int kFew = 256;                // entries of a group that are not divided any more
 constexpr int kRankSort = 256;           // entries up to which a list is sorted by counting
@@ -457,22 +457,23 @@ struct Row {
             if (MAX) s.warp_u64[0][warp] = (static_cast<u64>(bad) << 32) | __float_as_uint(top_);
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            a = b = 0.0;
-            int n = 0;
-            for (int w = 0; w < kSelWarps; ++w) {
-                a += s.warp_f64[0][w];
-                b += s.warp_f64[1][w];
-                n += s.warp_int[w];
-                if (MAX) {
-                    top_ = fmaxf(top_, __uint_as_float(static_cast<uint32_t>(s.warp_u64[0][w])));
-                    bad |= static_cast<int>(s.warp_u64[0][w] >> 32);
-                }
+        if (warp == 0) {                                          // the warps' parts, a lane each
+            const bool some = lane < kSelWarps;
+            a = warp_sum(some ? s.warp_f64[0][lane] : 0.0);
+            b = warp_sum(some ? s.warp_f64[1][lane] : 0.0);
+            const int n = __reduce_add_sync(0xffffffffu, some ? s.warp_int[lane] : 0);
+            if (MAX) {
+                const u64 of = some ? s.warp_u64[0][lane] : static_cast<u64>(__float_as_uint(-INFINITY));
+                top_ = __uint_as_float(static_cast<uint32_t>(of));
+                for (int o = 16; o > 0; o >>= 1) top_ = fmaxf(top_, __shfl_xor_sync(0xffffffffu, top_, o));
+                bad = __reduce_or_sync(0xffffffffu, static_cast<int>(of >> 32));
             }
-            s.pub[turn].sum[0] = a;
-            s.pub[turn].sum[1] = b;
-            s.pub[turn].count = n;
-            if (MAX) { s.pub[turn].top = top_; s.pub[turn].bad = bad; }
+            if (lane == 0) {
+                s.pub[turn].sum[0] = a;
+                s.pub[turn].sum[1] = b;
+                s.pub[turn].count = n;
+                if (MAX) { s.pub[turn].top = top_; s.pub[turn].bad = bad; }
+            }
         }
         sync();
         Totals t = {{0.0, 0.0}, 0.0, -INFINITY, 0, 0};
@@ -709,7 +710,7 @@ struct Row {
     // The n entries of a list that keep(entry) takes, moved together; their number to *counter.
     template <int CAP, typename F>
     static __device__ void compact(u64* list, int n, int* counter, F keep) {
-        constexpr int kMine = CAP / kSelThreads;
+        constexpr int kMine = (CAP + kSelThreads - 1) / kSelThreads;
         u64 o[kMine];
         unsigned taken = 0;
 #pragma unroll
@@ -1358,24 +1359,18 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
     const bool first_only = by_p && p == 0.f;
     const double want = first_only ? 0.0 : ud * t.sum[0];
     constexpr double kNone = 1e-290;                              // (entries of -inf may add up to a little less than that)
-    auto choose = [&](const double* sums, double left) {          // one thread
-        int chosen = -1;
-        double ahead = 0.0;
-        for (int w = 0; w < kSelWarps; ++w) {
-            if (sums[w] <= kNone) continue;
-            chosen = w;
-            s.found_mass = left - ahead;
-            if (left - ahead < sums[w]) break;
-            ahead += sums[w];
-        }
-        s.found[0] = chosen;
+    auto choose = [&](const double* sums, double left) {          // one warp, a lane per sum
+        const double of = lane < kSelWarps && sums[lane] > kNone ? sums[lane] : 0.0, until = warp_scan(of);
+        const unsigned some = __ballot_sync(0xffffffffu, of > 0.0), hit = __ballot_sync(0xffffffffu, of > 0.0 && left < until);
+        const int chosen = hit != 0u ? __ffs(hit) - 1 : 31 - __clz(some);
+        if (lane == 0) s.found[0] = chosen;
+        if (lane == chosen) s.found_mass = left - (until - of);
     };
-    if (threadIdx.x == 0) {
-        double mine = 0.0;
-        for (int w = 0; w < kSelWarps; ++w) mine += s.warp_kept[w];
-        s.found[0] = -1;
+    if (warp == 0) {
+        const double mine = s.pub[r.turn ^ 1].sum[0];
         // (t.before of the next CTA is this one's t.before + mine, the same sum: one CTA takes it)
         if (want >= t.before && mine > kNone && want < t.before + mine) choose(s.warp_kept, want - t.before);
+        else if (lane == 0) s.found[0] = -1;
     }
     __syncthreads();
     const int owner = s.found[0];
@@ -1418,7 +1413,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
     __syncthreads();
     if (lane == 0) s.warp_f64[0][warp] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) choose(s.warp_f64[0], left);
+    if (warp == 0) choose(s.warp_f64[0], left);
     __syncthreads();
     if (s.found[0] != warp) return;
     left = s.found_mass;
