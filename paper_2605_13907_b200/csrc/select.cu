@@ -900,8 +900,8 @@ struct Row {
     // about `ref` in `full` (all threads of all CTAs).  -1: a list overflowed, or the sum says that the row needs a closer look.
     // What the pass lists is chunks, by their largest entry (a tenth of the instructions that listing entries takes; 613 x 151936
     // bf16, K = 64: 94 -> 78 us); the K-th largest of them bounds the K-th entry from below as well.
-    // 2,048 x 126464 fp32, K = 8: 205-229 us, 5.0 TB/s; K = 128: 272; 512 x 262144 fp16, K = 50: 89 us, 3.0 TB/s (the exponentials and maxima of
-    // 16-bit entries: 20 instructions per entry and lane before, about 12 now).
+    // 2,048 x 126464 fp32, K = 128: 254 us, 4.1 TB/s; 512 x 262144 fp16, K = 50: 90 us, 3.0 TB/s, bound by the instructions for 16-bit entries
+    // (15 per 32 of them, 20 with the entries listed).
     __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
         SelShared& s = smem();
         constexpr int kTile = kSelThreads * kDeep;
@@ -1518,8 +1518,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
 
 template <typename K>
 cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream, int forced /* CTAs per row at least, if the row is long enough */ = 0) {
-    // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  (Not beyond: the cluster's barriers and the
-    // merging cost more than a better filled last wave gives; 613 rows of 151936 bf16, K = 64: one CTA 109 us, four 349.)
+    // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  Not beyond: each has 20 to 50 us of
+    // barriers, merging and instruction fetches of its own (613 rows of 151936 bf16, K = 64: one CTA 76 us, two 102, four 186; 256 rows with
+    // top-p 171, 296, 485).
     int c = 1;
     while (c < kMaxCluster && rows * c * 2 <= 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
     if (forced > 0)
