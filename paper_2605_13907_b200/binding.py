@@ -706,7 +706,9 @@ def distill(shape: Shape, H, W, ids, logits, mask, kl, loss, workspace, temperat
                            ("weights", weights, torch.float32), ("lse", lse, torch.float32)):
         if t is not None:
             _check_rows(name, t, T, dtype, dev)
-    for t in (H, W, ids, logits, loss, dH, dW):
+    if loss is not None:
+        _check_rows("loss", loss, 1, torch.float32, dev)
+    for t in (H, W, ids, logits, dH, dW):
         if t is not None and t.device != dev:
             raise AisError("all tensors must live on the workspace's device")
     _check_status(dev_status, dev)

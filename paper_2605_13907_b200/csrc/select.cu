@@ -1132,7 +1132,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
     // a top-k of everything is none, unless it makes the whole of a short row the list that the other filters work on
     if (a.V > kMaxTopLogits) {
         if (k >= a.V) k = 0;
-    } else if (k <= 0 && (p < 1.f || m > 0.f)) {
+    } else if (k > a.V || (k <= 0 && (p < 1.f || m > 0.f))) {
         k = a.V;
     }
     if (a.rows_of != kAllRows && one_pass(k, p, m) != first_kind) return;
