@@ -897,7 +897,8 @@ struct Row {
     }
 
     // The K largest entries by one pass: rank 0 gets them sorted in s.list and returns their number, and the fp32 sum of exponentials
-    // about `ref` in `full` (all threads of all CTAs).  -1: a list overflowed, or the sum says that the row needs a closer look.
+    // about `ref`, the largest entry of a slice's first tile that has one, in `full` (all threads of all CTAs).  -1: a list overflowed, or the
+    // sum says that the row needs a closer look.
     // What the pass lists is chunks, by their largest entry (a tenth of the instructions that listing entries takes; 613 x 151936
     // bf16, K = 64: 94 -> 78 us); the K-th largest of them bounds the K-th entry from below as well.
     // 2,048 x 126464 fp32, K = 128: 254 us, 4.1 TB/s; 512 x 262144 fp16, K = 50: 90 us, 3.0 TB/s, bound by the instructions for 16-bit entries
@@ -911,20 +912,29 @@ struct Row {
         __syncthreads();
         uint4 raw[kDeep];
         float thr = -INFINITY;
-        ref = 0.f;
+        ref = -INFINITY;
         full = 0.0;
         bool overflow = false;
+        int first = 0;                                            // the first tile with an entry above -inf
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) raw[j] = chunk(c0 + j * kSelThreads + threadIdx.x, c1);
         if (n > 0) {
-            // a bound from the first tile.  Groups: the entries of a thread's first and of its last loads, of a thread, or of two threads
-            float half[2] = {-INFINITY, -INFINITY};
+            // Groups: the entries of a thread's first and of its last loads, of a thread, or of two threads.  Tiles of nothing but -inf are
+            // passed over: neither a bound nor a reference for the sum comes from them (a NaN stops the search and goes on into the sum).
+            float half[2];
+#pragma unroll 1
+            for (;; first += kTile) {
+                half[0] = half[1] = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < kDeep; ++j) {
-                float v[kEach];
-                Elem<T>::unpack(raw[j], v);
+                for (int j = 0; j < kDeep; ++j) {
+                    float v[kEach];
+                    Elem<T>::unpack(raw[j], v);
 #pragma unroll
-                for (int k = 0; k < kEach; ++k) half[j / (kDeep / 2)] = fmaxf(half[j / (kDeep / 2)], v[k]);
+                    for (int k = 0; k < kEach; ++k) half[j / (kDeep / 2)] = max_nan(half[j / (kDeep / 2)], v[k]);
+                }
+                if (__syncthreads_or(max_nan(half[0], half[1]) != -INFINITY) || first + kTile >= n) break;
+#pragma unroll
+                for (int j = 0; j < kDeep; ++j) raw[j] = chunk(c0 + first + (kDeep + j) * kSelThreads + threadIdx.x, c1);
             }
             float both = fmaxf(half[0], half[1]);
             int groups;
@@ -942,8 +952,22 @@ struct Row {
             }
             __syncthreads();
             thr = bound([&](int i) { return s.group_max[i]; }, groups, K, &ref);
-            if (!(fabsf(ref) < INFINITY)) ref = 0.f;
         }
+        if (ref == -INFINITY) {                                   // nothing but the ends of the row, if they
+            float v[kEach];
+            int i;
+            __syncthreads();
+            if (threadIdx.x < 2) s.group_max[threadIdx.x] = -INFINITY;
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0)
+                for (int tail = 0; tail < 2; ++tail)
+                    if (edge(tail != 0, threadIdx.x >> 5, v, i))
+                        for (int k = 0; k < kEach; ++k) s.group_max[tail] = fmaxf(s.group_max[tail], v[k]);
+            __syncthreads();
+            ref = fmaxf(s.group_max[0], s.group_max[1]);
+        }
+        const bool some = ref > -INFINITY;                        // of this slice (a tile of NaN alone leaves a reference of 0, and a sum of NaN)
+        if (!(fabsf(ref) < INFINITY)) ref = 0.f;
         // a chunk whose largest entry is above `above`: its place in the list
         auto push = [&](float most, int at_chunk) {
             const int at = atomicAdd(&s.list_n, 1);
@@ -964,15 +988,15 @@ struct Row {
             if (m > above) push(m, tail ? whole : -1);
             full += static_cast<double>(f);
         };
-        // (>= in the first tile, whose entries gave the bound; later ones of the same value come after K entries in the order)
+        // (>= in the tile whose entries gave the bound; later ones of the same value come after K entries in the order)
         const float first_above = thr > -INFINITY ? nextafterf(thr, -INFINITY) : -INFINITY;
         ends(false, first_above);
-        int tile = 0, limit = min(max(512, 4 * K), kChunkPrune);
+        int limit = min(max(512, 4 * K), kChunkPrune);
 #pragma unroll 1
-        for (int t0 = 0; t0 < n; t0 += kTile, ++tile) {
+        for (int t0 = first; t0 < n; t0 += kTile) {
             int pushed = 0;
             float f = 0.f;
-            const float above = tile == 0 ? first_above : thr;
+            const float above = t0 == first ? first_above : thr;
 #pragma unroll
             for (int j = 0; j < kDeep; ++j) {
                 float v[kEach];
@@ -1031,19 +1055,21 @@ struct Row {
         const int mine = overflow ? -1 : sort_top(s.list_few, K);
         if (C == 1) return mine;
         // the K largest of every slice, sorted together by rank 0
-        if (threadIdx.x == 0) { s.pub[turn].count = mine; s.pub[turn].top = ref; }
+        if (threadIdx.x == 0) { s.pub[turn].count = mine; s.pub[turn].top = some ? ref : -INFINITY; }
         sync();
         int at = 0, all = 0;
+        float most = -INFINITY;
         for (int r = 0; r < C; ++r) {
             const int k = remote(&s.pub[turn], r)->count;
             if (k < 0) overflow = true;
             if (r < rank) at += k;
             all += k;
+            most = fmaxf(most, remote(&s.pub[turn], r)->top);
         }
-        // every CTA's sum about the reference of rank 0
-        const float ref0 = remote(&s.pub[turn], 0)->top;
-        full *= exp2(static_cast<double>((ref - ref0) * c));
-        ref = ref0;
+        // every CTA's sum about the largest reference (one without an entry has 0, or NaN)
+        if (most == -INFINITY) most = 0.f;
+        if (some) full *= exp2((static_cast<double>(ref) - static_cast<double>(most)) * static_cast<double>(c));
+        ref = most;
         turn ^= 1;
         if (!overflow && rank != 0) {
             u64* list = remote(s.list, 0) + at;
