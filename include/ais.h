@@ -446,8 +446,8 @@ void ais_default_sampling(ais_sampling* how);   /* host pointer; fills in the nu
  *     lp[t]      = log(e_token / sum_S e)       log-prob under the distribution that was drawn from     (may be NULL)
  *     lp_full[t] = log(e_token / sum_v e_v)     log-prob at this temperature without the filters        (may be NULL)
  *     n_kept[t]  = |S|                                                                                  (may be NULL)
- * Temperature 0 draws the first entry of the order: lp = 0, lp_full at temperature 1.  The sums that decide are exact to about
- * 1e-12 of their size, whatever the type.  mask [rows] (may be NULL): rows with mask 0 give token -1 and zeros.  So do rows without
+ * Temperature 0 draws the first entry of the order: lp = 0, lp_full at temperature 1.  The sums that decide are good to
+ * 1e-12 of the row's kept mass, whatever the type.  mask [rows] (may be NULL): rows with mask 0 give token -1 and zeros.  So do rows without
  * a finite entry (AIS_FLAG_EMPTY), with a NaN or +inf (AIS_FLAG_NONFINITE) or with a parameter of their own out of range
  * (AIS_FLAG_PARAM); the numbers in `how` are checked on the host.
  * No workspace.  A row's token and n_kept do not depend on the other rows of the call, its log-probs to the last bits only (the

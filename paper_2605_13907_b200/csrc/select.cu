@@ -23,8 +23,10 @@
 //
 // Precision: which token is drawn and how many are kept are decided by comparing sums over the vocabulary with borders; fp32
 // sums (1e-7 relative) would decide one row in a hundred differently.  Exponentials and sums that decide are fp64, summed in an
-// order that the sizes fix.  Sums by atomics (masses of bins) are 64-bit integers, exponentials rounded to multiples of 2^-44: exact to
-// add in any order, so no result depends on the order of atomics.
+// order that the sizes fix.  Sums by atomics (masses of parts of a group) are 96-bit integers, exponentials cut to multiples of 2^-76: exact to
+// add in any order, so no result depends on the order of atomics, and of 327,680 entries off by 2^-57 at most.  (In 64 bits, multiples of
+// 2^-44, entries of one value are all off by the same amount: 300,000 of them at e^-22 by eight entries' mass.)  The 1,024 masses of a list have
+// multiples of 2^-53 in 64 bits.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -58,7 +60,8 @@ constexpr int kRankSort = 256;           // entries up to which a list is sorted
 constexpr int kMaxCluster = 8;
 constexpr float kBinsPerNat = 256.f;
 constexpr int kIndexBits = 20;
-constexpr double kMassOne = 17592186044416.0;   // 2^44
+constexpr double kMassOne = 17592186044416.0;       // 2^44: units of a Mass's upper word
+constexpr double kListOne = 9007199254740992.0;     // 2^53: units of a list's masses
 constexpr int kTableCopies = 16;         // of the table of powers of two
 
 constexpr float kTwo23 = 8388608.f;
@@ -83,13 +86,17 @@ struct alignas(16) SelShared {
     union {
         uint32_t tot[kBins];             // of the row (more than one CTA)
         struct {
-            u64 mass[kSplit];            // dividing a group: masses and counts of this CTA, of the row (more than one CTA)
-            u64 mass_tot[kSplit];
+            uint32_t mass[3][kSplit];    // dividing a group: masses (lowest word first) and counts of this CTA, of the row (more than one CTA)
+            uint32_t mass_tot[3][kSplit];
             uint32_t part[kSplit];
             uint32_t part_tot[kSplit];
-            u64 few[kFew];               // the last entries of a group
-            u64 few_mass[kFew];
         };
+        struct {
+            u64 few[kFew];               // the last entries of a group
+            u64 few_hi[kFew];            // and their masses
+            uint32_t few_lo[kFew];
+        };
+        u64 list_mass[kMaxTopLogits];    // of the entries of a sorted list
         struct {
             uint32_t small_hist[kSelThreads];
             float group_max[2 * kSelThreads];
@@ -98,7 +105,7 @@ struct alignas(16) SelShared {
     };
     double exp2_table[64 * kTableCopies];   // 2^(j / 64)
     double warp_kept[kSelWarps];         // kept mass of every warp's range
-    u64 warp_listed[kSelWarps];          // what the list adds to it
+    uint32_t warp_listed[3][kSelWarps];  // what the list adds to it
     Published pub[2];                    // in turn, so that one barrier per exchange is enough
     double warp_f64[2][kSelWarps];
     u64 warp_u64[2][kSelWarps];
@@ -196,14 +203,26 @@ __device__ __forceinline__ float ex2_approx(float x) {
     return y;
 }
 
-// A 64-bit sum in shared memory by two 32-bit atomics: a 64-bit one is a loop of compare-and-swaps, which takes 300 us for the 2,000
-// entries of one value that share a sum.
-__device__ __forceinline__ void add_u64(u64* sum, u64 v) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(sum);
-    const uint32_t lo = static_cast<uint32_t>(v), old = atomicAdd(w, lo);
-    const uint32_t hi = static_cast<uint32_t>(v >> 32) + (old + lo < old ? 1u : 0u);
-    if (hi != 0u) atomicAdd(w + 1, hi);
+// An exponential as a multiple of 2^-76, at most 2^76; 2^20 of them add up to 96 bits at most.
+struct Mass {
+    u64 hi;                  // multiples of 2^-44
+    uint32_t lo;
+};
+// A sum of upper and one of lower words in units of 2^-44.  Rounded, but rising with the exact sum, so that the end of one part and the start
+// of the next are the same number.
+__device__ __forceinline__ double in_units(u64 hi, u64 lo) {
+    return static_cast<double>(hi + (lo >> 32)) + static_cast<double>(static_cast<uint32_t>(lo)) * 0x1p-32;
 }
+// A 96-bit sum in shared memory (words `stride` apart, the lowest first) by 32-bit atomics, each adding what its word carries: a 64-bit atomic is
+// a loop of compare-and-swaps, which takes 300 us for the 2,000 entries of one value that share a sum.
+__device__ __forceinline__ void add_mass(uint32_t* sum, int stride, Mass m) {
+    const uint32_t old = atomicAdd(sum, m.lo);
+    const u64 mid = (m.hi & 0xffffffffull) + (old + m.lo < old ? 1u : 0u);
+    const uint32_t mid_lo = static_cast<uint32_t>(mid), old_mid = atomicAdd(sum + stride, mid_lo);
+    const uint32_t hi = static_cast<uint32_t>(m.hi >> 32) + static_cast<uint32_t>(mid >> 32) + (old_mid + mid_lo < old_mid ? 1u : 0u);
+    if (hi != 0u) atomicAdd(sum + 2 * stride, hi);
+}
+__device__ __forceinline__ u64 upper_words(const uint32_t* sum, int stride) { return static_cast<u64>(sum[2 * stride]) << 32 | sum[stride]; }
 
 template <typename N>
 __device__ __forceinline__ N warp_sum(N v) {
@@ -404,10 +423,16 @@ struct Row {
         }
         return __uint_as_float(lo ^ ((lo >> 31) != 0u ? 0x80000000u : 0xffffffffu));
     }
-    __device__ __forceinline__ u64 mass(float v) const { return __double2ull_rn(weight(smem().exp2_table, v) * kMassOne); }
+    __device__ __forceinline__ Mass mass(float v) const {
+        const double w = weight(smem().exp2_table, v) * kMassOne;
+        Mass m;
+        m.hi = __double2ull_rd(w);
+        m.lo = __double2uint_rd((w - static_cast<double>(m.hi)) * 0x1p32);
+        return m;
+    }
     __device__ __forceinline__ const uint32_t* counts() const { return C > 1 ? smem().tot : smem().hist; }
     __device__ __forceinline__ const uint32_t* parts() const { return C > 1 ? smem().part_tot : smem().part; }
-    __device__ __forceinline__ const u64* masses() const { return C > 1 ? smem().mass_tot : smem().mass; }
+    __device__ __forceinline__ const uint32_t* masses() const { return C > 1 ? smem().mass_tot[0] : smem().mass[0]; }
 
     __device__ void clear_hist() const {
         SelShared& s = smem();
@@ -423,6 +448,26 @@ struct Row {
             N c = 0;
             for (int r = 0; r < C; ++r) c += remote(mine, r)[b];
             for (int r = 0; r < C; ++r) remote(total, r)[b] = c;
+        }
+    }
+    __device__ void merge_masses() const {
+        SelShared& s = smem();
+        const int share = kSplit / C;
+        for (int i = threadIdx.x; i < share; i += kSelThreads) {
+            const int b = rank * share + i;
+            u64 hi = 0, lo = 0;
+            for (int r = 0; r < C; ++r) {
+                const uint32_t* m = remote(s.mass[0], r) + b;
+                hi += upper_words(m, kSplit);
+                lo += m[0];
+            }
+            hi += lo >> 32;
+            for (int r = 0; r < C; ++r) {
+                uint32_t* m = remote(s.mass_tot[0], r) + b;
+                m[0] = static_cast<uint32_t>(lo);
+                m[kSplit] = static_cast<uint32_t>(hi);
+                m[2 * kSplit] = static_cast<uint32_t>(hi >> 32);
+            }
         }
     }
     __device__ void merge_hist() const {
@@ -518,18 +563,24 @@ struct Row {
         if (threadIdx.x == 0) s.found[3] = 0;
         constexpr int kMine = kSplit / kSelThreads;
         const int b0 = threadIdx.x * kMine;
-        u64 m[kMine], sum = 0, total;
-        for (int j = 0; j < kMine; ++j) sum += m[j] = masses()[b0 + j];
-        u64 before = block_scan(sum, s.warp_u64[0], total);
+        const uint32_t* lo_of = masses();
+        u64 hi = 0, lo = 0, total;
         for (int j = 0; j < kMine; ++j) {
-            const double lo = mass0 + static_cast<double>(before), hi = mass0 + static_cast<double>(before + m[j]);
-            if (m[j] != 0 && lo < target && hi >= target) {
+            hi += upper_words(lo_of + b0 + j, kSplit);
+            lo += lo_of[b0 + j];
+        }
+        hi = block_scan(hi, s.warp_u64[0], total);
+        lo = block_scan(lo, s.warp_u64[1], total);
+        for (int j = 0; j < kMine; ++j) {
+            const double from = mass0 + in_units(hi, lo);
+            hi += upper_words(lo_of + b0 + j, kSplit);
+            lo += lo_of[b0 + j];
+            if (from < target && mass0 + in_units(hi, lo) >= target) {
                 s.found[0] = b0 + j;
                 s.found[2] = parts()[b0 + j];
                 s.found[3] = 1;
-                s.found_mass = lo;
+                s.found_mass = from;
             }
-            before += m[j];
         }
         __syncthreads();
     }
@@ -764,7 +815,7 @@ struct Row {
             if (ends && (threadIdx.x & 31) == 0) { s.warp_u64[0][threadIdx.x >> 5] = lo; s.warp_u64[1][threadIdx.x >> 5] = hi; }
             for (int b = threadIdx.x; b < kSplit; b += kSelThreads) {
                 s.part[b] = 0;
-                if (MASS) s.mass[b] = 0;
+                if (MASS) s.mass[0][b] = s.mass[1][b] = s.mass[2][b] = 0;
             }
             __syncthreads();
             if (ends) {
@@ -786,12 +837,12 @@ struct Row {
                 if (o < lo || o > hi) return;
                 const int b = static_cast<int>((o - lo) >> shift);
                 atomicAdd(&s.part[b], 1u);
-                if (MASS) add_u64(&s.mass[b], mass(x));
+                if (MASS) add_mass(&s.mass[0][b], kSplit, mass(x));
             });
             sync();
             if (C > 1) {
                 merge(s.part, s.part_tot, kSplit);
-                if (MASS) merge(s.mass, s.mass_tot, kSplit);
+                if (MASS) merge_masses();
                 sync();
             }
             if (MASS) {
@@ -820,19 +871,26 @@ struct Row {
         if (rank == 0) {
             const int n = min(s.list_few, kFew);
             const u64 o = threadIdx.x < n ? s.few[threadIdx.x] : 0;
-            const u64 m = MASS && threadIdx.x < n ? mass(value_of(o)) : 1;
-            if (threadIdx.x < n) s.few_mass[threadIdx.x] = m;
+            const Mass m = MASS && threadIdx.x < n ? mass(value_of(o)) : Mass{1, 0};
+            if (threadIdx.x < n) {
+                s.few_hi[threadIdx.x] = m.hi;
+                s.few_lo[threadIdx.x] = m.lo;
+            }
             if (threadIdx.x == 0) s.pub[turn].lo = n > 0 ? 0 : last_finite();
             __syncthreads();
             if (threadIdx.x < n) {
-                u64 before = 0;
+                u64 before = 0, before_lo = 0;
                 bool is_last = true;
                 for (int i = 0; i < n; ++i) {
                     const u64 other = s.few[i];
-                    if (other < o) before += s.few_mass[i];
-                    else if (other > o) is_last = false;
+                    if (other < o) {
+                        before += s.few_hi[i];
+                        before_lo += s.few_lo[i];
+                    } else if (other > o) {
+                        is_last = false;
+                    }
                 }
-                const double lo = mass0 + static_cast<double>(before), hi = mass0 + static_cast<double>(before + m);
+                const double lo = mass0 + in_units(before, before_lo), hi = mass0 + in_units(before + m.hi, before_lo + m.lo);
                 const bool cut = MASS ? (lo < target && hi >= target) || (is_last && hi < target) : before + 1 == static_cast<u64>(want);
                 if (cut) s.pub[turn].lo = o;
             }
@@ -1091,11 +1149,11 @@ __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Writ
     SelShared& s = smem();
     constexpr int kMine = kMaxTopLogits / kSelThreads;
     r.set_scale(value_of(s.list[0]), r.inv_t);
-    u64* w_of = s.mass;
-    static_assert(kSplit >= kMaxTopLogits, "masses of the list");
+    u64* w_of = s.list_mass;
+    auto mass = [&](float v) { return __double2ull_rn(r.weight(s.exp2_table, v) * kListOne); };
     u64 w[kMine], mine = 0, total;
     const int i0 = threadIdx.x * kMine;
-    for (int j = 0; j < kMine; ++j) mine += w[j] = i0 + j < n ? r.mass(value_of(s.list[i0 + j])) : 0;
+    for (int j = 0; j < kMine; ++j) mine += w[j] = i0 + j < n ? mass(value_of(s.list[i0 + j])) : 0;
     u64 cum = block_scan(mine, s.warp_u64[0], total);
     const double target = static_cast<double>(p) * static_cast<double>(total), md = m;
     int kept = 0;
@@ -1119,7 +1177,7 @@ __device__ void draw_from_list(Row<T>& r, int n, float p, float m, float u, Writ
         u64 c = 0;
         for (int j = 0; j < n_kept; ++j)
             if (index_of(s.list[j]) < v) c += w_of[j];
-        if (c <= t && t < c + w_of[i]) write(s.list[i], log(static_cast<double>(total) / kMassOne), n_kept);
+        if (c <= t && t < c + w_of[i]) write(s.list[i], log(static_cast<double>(total) / kListOne), n_kept);
     }
 }
 
@@ -1269,7 +1327,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
         }
         double above = 0.0;                                       // kept mass (this thread's part)
         bool counted = false;                                     // kept holds the entries that `above` and the lists sum up
-        if (threadIdx.x < kSelWarps) s.warp_listed[threadIdx.x] = 0;
+        if (threadIdx.x < 3 * kSelWarps) s.warp_listed[0][threadIdx.x] = 0;
         if (by_p) {
             if (by_k) {                                           // the histogram of what top-k has left
                 __syncthreads();
@@ -1336,7 +1394,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
                         counted = true;
                         listed([&](float x, u64 o) {
                             if (o > cut) return;
-                            add_u64(&s.warp_listed[r.warp_of(index_of(o))], r.mass(x));
+                            add_mass(&s.warp_listed[0][r.warp_of(index_of(o))], kSelWarps, r.mass(x));
                             ++kept;
                         });
                         if (r.rank == 0 && threadIdx.x == 0) kept += before;
@@ -1370,7 +1428,7 @@ __device__ __forceinline__ void sample_row(const SelectArgs& a) {
             });
         }
         __syncthreads();
-        const double of_warp = warp_sum(above) + static_cast<double>(s.warp_listed[warp]) / kMassOne;
+        const double of_warp = warp_sum(above) + in_units(upper_words(&s.warp_listed[0][warp], kSelWarps), s.warp_listed[0][warp]) / kMassOne;
         if (lane == 0) s.warp_kept[warp] = of_warp;
         t = r.template add_up<false>(lane == 0 ? of_warp : 0.0, full, kept, 0.f, 0);
         log_full = log(t.sum[1]);
