@@ -485,7 +485,8 @@ int ais_top_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64
  * dH [T, ldh] bf16 (may be NULL), dW in W's layout with row stride lddw, bf16 (may be NULL; rounded once from fp32 sums over the
  * whole batch, which has to fit the workspace).  Without dW the forward pass leaves the exponentials of its logits in scratch rows and
  * the two tensor-core passes are all there is; dW needs the scratch in its final scale, so with it the forward pass leaves 16-bit
- * codes of the logits (off by 1/1280 at most, 8e-4 of an exponential) that a sweep turns into it.
+ * codes of the logits (off by 1/1280 at most, 8e-4 of an exponential; an entry whose logit lies below -42 counts for nothing, which rows
+ * of lse >= -5 do not miss) that a sweep turns into it; rows of lse outside [-5, 59] are computed again.
  * The tensor cores cut, not round, the partial sums of a contraction, which makes logits a few 1e-6 of their size too small in
  * the mean (1.6e-8 per 16 terms, measured); the factor 1 / tau carries the correction.
  */

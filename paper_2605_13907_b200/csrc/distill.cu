@@ -9,7 +9,8 @@
 //     kl = M sum r (log r + log M - x + lse),   d kl / d x_v = M (p_v - sum_{k: id_k = v} r_k).
 // The gradient off the listed columns is M p_v = M e^-lse e^x_v: the scratch keeps the e^x that the forward pass leaves (exp_form
 // in lmhead.cuh), the listed columns become (p_v - r_v) e^lse, the difference formed in fp64 before its one rounding to bf16, and
-// the dH pass scales the row by w M e^-lse / tau.  Rows whose lse is out of that form's range are recomputed in plain form.
+// the dH pass scales the row by w M e^-lse / tau.  With dW the scratch is plain, coef (p - r), from 16-bit codes of the logits (code_form).  Rows
+// whose lse is out of their form's range are recomputed in plain form.
 #include <cuda_fp16.h>
 
 #include "../../include/ais.h"
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                 // the row's factor, and what the scratch holds at the listed columns: (p - r) e^lse, or coef (p - r)
                 if (a.scale) scale = kept ? static_cast<float>(w * mass * a.inv_tau * exp(-lse)) : 1.f;
                 const double f = kept ? exp(lse) : w * mass * a.inv_tau;
-                if (a.redo && !exp_form(lse_out) && coef != 0.f && lane == 0) {
+                if (a.redo && !(a.scale ? exp_form(lse_out) : code_form(lse_out)) && coef != 0.f && lane == 0) {
                     a.redo_flags[t / kBM] = 1;
                     atomicAdd(a.redo_count, 1u);
                 }

@@ -106,8 +106,10 @@ __device__ __forceinline__ float exp_form_target(float lp, float lse) { return e
 // in the final scale, coef e^(x - lse), and lse is known only when the logits are gone.  A code is off by 1/1280 at most, so its
 // exponential by 8e-4 (4.5e-4 rms, beside the 1.7e-3 of the bf16 that it becomes), and turning codes into scratch is one sweep of 4 bytes per
 // entry where computing the logits again is 2 d multiply-adds: 0.25 against 2.2 ms for 2,305 rows, d = 4096, V = 151936.  Rows
-// outside exp_form's range of lse, whose logits leave that of the codes, are computed again.
+// whose logits would leave the range of the codes are computed again: above, an lse of 59 keeps every logit below 60.4; below, an lse of -5
+// leaves entries of a probability under e^-37 = 8.5e-17 out, 3e-11 of a row of 327,680 together.
 constexpr float kCodeSteps = 640.f, kCodeZero = 42.f;
+__host__ __device__ inline bool code_form(float lse) { return lse >= -5.0f && lse <= 59.0f; }
 
 // Pacing of the CTAs of a launch (lmhead_common.cuh): stage fills per announcement, counters in the ring.
 constexpr int kPaceFills = 16;
