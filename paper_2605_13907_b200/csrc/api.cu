@@ -1194,7 +1194,7 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
     job.lse = lse;
     job.row_lse = reinterpret_cast<float*>(ws + L.off_lse);
     job.coef = reinterpret_cast<float*>(ws + L.off_coef);
-    job.scale = keep ? reinterpret_cast<float*>(ws + L.off_scale) : nullptr;
+    job.scale = reinterpret_cast<float*>(ws + L.off_scale);
     job.U = keep ? U : nullptr;
     job.ldU = L.ldU;
     job.redo = grads != 0;
@@ -1263,13 +1263,14 @@ int ais_distill(const ais_shape* shape, const void* H, const void* W, int32_t K,
             return AIS_ERR_DEVICE;
         a.lse = job.row_lse;
         a.coef = job.coef;
-        a.row_scale = job.scale;
+        a.row_scale = keep ? job.scale : nullptr;
         a.tile_active = ws + L.off_redo;
         a.gate = job.redo_count;
         if (logits_pass(dv ? kBwdPPickDv : kBwdPPick) != cudaSuccess) return AIS_ERR_DEVICE;
         if (dH) {
             a.dH = static_cast<__nv_bfloat16*>(dH);
             a.lddh = shape->ldh;
+            a.row_scale = job.scale;
             if (enqueue_dh(a, shape, L, ws, tmU, tmW_n, num_sms, pass, s) != cudaSuccess) return AIS_ERR_DEVICE;
         }
         if (dW) {

@@ -151,11 +151,11 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                 kl = static_cast<float>(sum);
                 contribution = w * sum;
                 coef = static_cast<float>(w * mass * a.inv_tau);
-                const bool kept = a.scale != nullptr && exp_form(lse_out);
+                const bool kept = a.U != nullptr && exp_form(lse_out);
                 // the row's factor, and what the scratch holds at the listed columns: (p - r) e^lse, or coef (p - r)
-                if (a.scale) scale = kept ? static_cast<float>(w * mass * a.inv_tau * exp(-lse)) : 1.f;
+                scale = kept ? static_cast<float>(w * mass * a.inv_tau * exp(-lse)) : 1.f;
                 const double f = kept ? exp(lse) : w * mass * a.inv_tau;
-                if (a.redo && !(a.scale ? exp_form(lse_out) : code_form(lse_out)) && coef != 0.f && lane == 0) {
+                if (a.redo && !(a.U ? exp_form(lse_out) : code_form(lse_out)) && coef != 0.f && lane == 0) {
                     a.redo_flags[t / kBM] = 1;
                     atomicAdd(a.redo_count, 1u);
                 }
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                     for (; j < a.K && a.ids[at + j] == id; ++j) r += exp(static_cast<double>(a.logits[at + j]) * a.inv_tau - lse_k);
                     const float v = static_cast<float>((exp(static_cast<double>(a.pick[at + k]) - lse) - r) * f);
                     a.pick[at + k] = v;
-                    if (kept && a.U) a.U[lrow * a.ldU + id] = __float2bfloat16(v);
+                    if (kept) a.U[lrow * a.ldU + id] = __float2bfloat16(v);
                 }
             }
         }
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
             if (a.lse) a.lse[t] = lse_out;
             a.row_lse[t] = lse_out;
             a.coef[t] = coef;
-            if (a.scale) a.scale[t] = coef != 0.f ? scale : 0.f;
+            a.scale[t] = coef != 0.f ? scale : 0.f;
         }
     }
     // the loss: rows of a block in order, then the blocks in order, by the block that finishes last

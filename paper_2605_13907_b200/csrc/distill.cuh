@@ -46,10 +46,10 @@ struct DistillJob {
     float *kl, *lse;           // lse may be NULL
     float* row_lse;            // [T] workspace: lse of every row, for the recompute pass
     float* coef;               // [T] workspace: w M / tau
-    float* scale;              // [T] factor of the row in the dH pass; NULL: the scratch is in plain form everywhere
-    __nv_bfloat16* U;          // scratch of this launch's rows in exponent form (with scale), else NULL
+    float* scale;              // [T] factor of the row in the dH pass: 0 where there is no gradient (the row's scratch may meet a NaN in W)
+    __nv_bfloat16* U;          // scratch of this launch's rows in exponent form; NULL: codes, or no scratch
     int64_t ldU;
-    bool redo;                 // row tiles with a row outside exp_form are marked (with scale, and with codes in the scratch)
+    bool redo;                 // row tiles with a row outside the form of the scratch are marked
     uint8_t* redo_flags;       // per row tile of the batch, zeroed before
     uint32_t* redo_count;
     double* partials;          // [ceil(T / kDistillRows)]
