@@ -12,6 +12,7 @@
 // the dH pass scales the row by w M e^-lse / tau.  With dW the scratch is plain, coef (p - r), from 16-bit codes of the logits (code_form).  Rows
 // whose lse is out of their form's range are recomputed in plain form.
 #include <cuda_fp16.h>
+#include <float.h>
 
 #include "../../include/ais.h"
 #include "distill.cuh"
@@ -151,11 +152,13 @@ __global__ void __launch_bounds__(kDistillRows * 32) distill_rows_kernel(const _
                 kl = static_cast<float>(sum);
                 contribution = w * sum;
                 coef = static_cast<float>(w * mass * a.inv_tau);
-                const bool kept = a.U != nullptr && exp_form(lse_out);
-                // the row's factor, and what the scratch holds at the listed columns: (p - r) e^lse, or coef (p - r)
-                scale = kept ? static_cast<float>(w * mass * a.inv_tau * exp(-lse)) : 1.f;
+                // the row's factor, and what the scratch holds at the listed columns: (p - r) e^lse, or coef (p - r).  A factor that fp32
+                // would cut to a few bits (|w| M / tau below 5e-13 at an lse of 59) leaves the row to the plain form, which is factor 1.
+                const double factor = w * mass * a.inv_tau * exp(-lse);
+                const bool kept = a.U != nullptr && exp_form(lse_out) && fabs(factor) >= static_cast<double>(FLT_MIN);
+                scale = kept ? static_cast<float>(factor) : 1.f;
                 const double f = kept ? exp(lse) : w * mass * a.inv_tau;
-                if (a.redo && !(a.U ? exp_form(lse_out) : code_form(lse_out)) && coef != 0.f && lane == 0) {
+                if (a.redo && !(a.U ? kept : code_form(lse_out)) && coef != 0.f && lane == 0) {
                     a.redo_flags[t / kBM] = 1;
                     atomicAdd(a.redo_count, 1u);
                 }

@@ -232,7 +232,8 @@ __device__ __forceinline__ RowState begin_row(const LmheadArgs& a, int64_t lrow,
         const float lse = a.lse[r.grow];
         r.mul = a.coef[r.grow];
         if (r.mul == 0.f) r.valid = false;             // rows without gradient are written as exact zeros
-        r.ef = a.row_scale != nullptr && exp_form(lse);
+        // (distillation: a row of factor 1 is plain, or, with w M e^-lse / tau = 1, the same in both forms)
+        r.ef = a.row_scale != nullptr && exp_form(lse) && !(pick_mode(MODE) && a.row_scale[r.grow] == 1.f);
         if (r.ef) { r.mul = 1.f; r.target = pick_mode(MODE) ? 0.f : exp_form_target(a.lp[r.grow], lse); }
         else r.off2 = lse * kLog2e;
     }
