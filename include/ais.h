@@ -487,8 +487,10 @@ int ais_top_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64
  * the two tensor-core passes are all there is; dW needs the scratch in its final scale, so with it the forward pass leaves 16-bit
  * codes of the logits (off by 1/1280 at most, 8e-4 of an exponential; an entry whose logit lies below -42 counts for nothing, which rows
  * of lse >= -5 do not miss) that a sweep turns into it; rows of lse outside [-5, 59] are computed again.
- * The tensor cores cut, not round, the partial sums of a contraction, which makes logits a few 1e-6 of their size too small in
- * the mean (1.6e-8 per 16 terms, measured); the factor 1 / tau carries the correction.
+ * The tensor cores cut, not round, the partial sums of a contraction, which makes logits too small by 1.6e-8 of their size per 16 terms in
+ * the mean (hidden units in no particular order); the factor 1 / tau takes that back.  A logit is off by up to 2^-23 of its largest
+ * partial sum per 16 terms with it as without it, and it makes lse larger than that of ais_logprob_fwd, which has no such factor, by
+ * 1.6e-8 d / 16 sum_v p_v x_v.
  */
 #define AIS_DISTILL_DH 1u
 #define AIS_DISTILL_DW 2u
