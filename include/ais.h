@@ -451,7 +451,8 @@ void ais_default_sampling(ais_sampling* how);   /* host pointer; fills in the nu
  * a finite entry (AIS_FLAG_EMPTY), with a NaN or +inf (AIS_FLAG_NONFINITE) or with a parameter of their own out of range
  * (AIS_FLAG_PARAM); the numbers in `how` are checked on the host.
  * No workspace.  A row's token and n_kept do not depend on the other rows of the call, its log-probs to the last bits only (the
- * number of rows decides how many CTAs share one, and so the order of its sums).
+ * number of rows decides how many CTAs share one, and so the order of its sums).  lp comes from the fp64 sums; lp_full, like lse below, from fp32
+ * exponentials and partial sums wherever a filter is on: good to 1.5e-5.
  */
 int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t ld, const ais_sampling* how, const float* u,
                const uint8_t* mask, int32_t* tokens, float* lp, float* lp_full, int32_t* n_kept, uint32_t* dev_status, void* stream);
@@ -482,6 +483,9 @@ int ais_top_logits(const void* logits, int dtype, int64_t rows, int64_t V, int64
  * count for nothing, an id beyond V likewise (AIS_FLAG_TOKEN_RANGE), an id given twice counts twice.  Rows with mask 0, without
  * an entry, or with non-finite teacher or student values (AIS_FLAG_NONFINITE; lse = NaN) give kl 0 and a zero row of dH.
  * kl [T] float; lse [T] = log sum_v exp(x_v) (may be NULL); loss: one float (may be NULL).
+ * The factors p_v - sum r_k of the gradients, formed in fp64 at the listed entries, are rounded to bf16 before the contractions that make dH and
+ * dW of them (the tensor cores take 16-bit operands), and dH and dW are rounded once more: 2.3e-3 of their norm, where the second rounding alone
+ * makes 1.7e-3.
  * dH [T, ldh] bf16 (may be NULL), dW in W's layout with row stride lddw, bf16 (may be NULL; rounded once from fp32 sums over the
  * whole batch, which has to fit the workspace).  Without dW the forward pass leaves the exponentials of its logits in scratch rows and
  * the two tensor-core passes are all there is; dW needs the scratch in its final scale, so with it the forward pass leaves 16-bit

@@ -3,9 +3,12 @@
 // between two of them.  What a kernel may rely on, and what it owes the next one:
 //  - Every kernel triggers (pdl_trigger) only after its own wait.  So when a kernel starts, everything older than the kernel
 //    before it is complete, and it may read that before its wait (the moments and rectification kernels read row offsets,
-//    masks and log-probs so early); it may write nothing to global memory before it.  The one exception is a pass that runs
-//    beside the other pass of its call (LmheadArgs::overlap): it triggers at once and waits at its end, and the merge behind
-//    it reads nothing early.
+//    masks and log-probs so early); it may write nothing to global memory before it.  Two kernels are exceptions: they run beside
+//    the kernel before them, trigger at once and wait at their end, so what THAT kernel writes is not complete either when the next one
+//    starts.  One is a pass that runs beside the other pass of its call (LmheadArgs::overlap); the merge behind it reads nothing early.  The
+//    other is the second launch of a sampling call with filters per row (SelectArgs::late), which may stand before any call of the
+//    library: the first kernel of a call may therefore not read early what a sampling call writes (tokens, log-probs, counts, a status
+//    word).  Those that open a call all wait first.
 //  - What the kernel before it writes it reads after the wait, and not through pointers that promise the data constant for as
 //    long as the kernel runs (const together with __restrict__, __ldg): the writer may run beside it.
 //  - Every thread waits before it returns, so that a kernel's completion implies the completion of everything before it.

@@ -959,8 +959,8 @@ struct Row {
     // sum says that the row needs a closer look.
     // What the pass lists is chunks, by their largest entry (a tenth of the instructions that listing entries takes; 613 x 151936
     // bf16, K = 64: 94 -> 78 us); the K-th largest of them bounds the K-th entry from below as well.
-    // 2,048 x 126464 fp32, K = 128: 254 us, 4.1 TB/s; 512 x 262144 fp16, K = 50: 90 us, 3.0 TB/s, bound by the instructions for 16-bit entries
-    // (15 per 32 of them, 20 with the entries listed).
+    // 2,048 x 126464 fp32, K = 128: 248 us, 4.2 TB/s; 512 x 262144 fp16, K = 50: 88 us, 3.1 TB/s, bound by instructions and barriers: 15 instructions
+    // per 32 of the 16-bit entries (20 with the entries listed), of which the loop over the tiles has six or so, bounds and sorting the rest.
     __device__ int stream_top(int K, double inv_t_, float& ref, double& full) const {
         SelShared& s = smem();
         constexpr int kTile = kSelThreads * kDeep;
@@ -1603,8 +1603,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) top_logits_kernel(const __grid
 template <typename K>
 cudaError_t launch_select(K kernel, SelectArgs& a, int64_t rows, int es, cudaStream_t stream, int forced /* CTAs per row at least, if the row is long enough */ = 0) {
     // More CTAs per row while all of them still run at once, two per SM, and a slice keeps 16 KB.  Not beyond: each has 20 to 50 us of
-    // barriers, merging and instruction fetches of its own (613 rows of 151936 bf16, K = 64: one CTA 76 us, two 102, four 186; 256 rows with
-    // top-p 171, 296, 485).
+    // barriers, merging and instruction fetches of its own (613 rows of 151936 bf16, K = 64: one CTA 78 us, two 104, four 189; 256 rows with
+    // top-p 175, 225, 304; unfiltered 66, 71, 80).
     int c = 1;
     while (c < kMaxCluster && rows * c * 2 <= 2 * 148 && static_cast<int64_t>(a.V) * es >= static_cast<int64_t>(c) * 2 * 16384) c *= 2;
     if (forced > 0)
@@ -1692,9 +1692,10 @@ int ais_sample(const void* logits, int dtype, int64_t rows, int64_t V, int64_t l
                : dtype == AIS_F16 ? launch_select(sample_kernel<__half>, a, rows, 2, s, forced)
                                   : launch_select(sample_kernel<float>, a, rows, 4, s, forced);
     };
-    // Rows with filters of their own: the few that need several passes get two CTAs each at least, in a launch of their own that the
-    // others overlap (256 x 151936 bf16 with mixed parameters and banned entries: 127 us, with four CTAs 133; in one launch with a CTA
-    // per row it took as long as its slowest row, 200).
+    // Rows with filters of their own: those that need several passes get two CTAs each at least, in a launch of their own that the others
+    // overlap.  The host does not see how many they are, and the rule is made for few of them.  151936 bf16, top-p 0.95 in an eighth, in half and
+    // in all of the rows, two CTAs against one: 256 rows 135, 170, 225 us against 165, 187, 175; 512 rows 202, 314, 401 against 260, 262, 347.  A
+    // batch of one kind pays 1 to 6 us for the launch that finds nothing to do.
     cudaError_t e = cudaSuccess;
     if (how->top_k_rows || how->top_p_rows || how->min_p_rows) {
         a.rows_of = kManyPasses;
